@@ -370,6 +370,136 @@ int pl_simulate_reward_ex(pl_graph_batch *g, int32_t D, const float *node_feats,
                           float *out_reward, float *out_runtime, float *out_peak_mem, int32_t *out_events,
                           void *stream);
 
+/* ---- losses on rows of logits: scoring of recorded decisions, the clipped policy loss and the
+ * preference loss, with the gradient of the logits.  A row is one decision: the logits of its
+ * actions and the action taken.  The logits may be those of this library's policy (pl_episode_run with
+ * keep_logits: [T, B, D], rows in the order PL_ROWS_BY_STEP) or any other network's, up to
+ * vocabularies of millions of tokens.
+ *
+ * Numbers: probabilities are taken in fp32 from logits of any type, sums over rows in float64;
+ * gradients are rounded once to the logits' type.  Summation orders are fixed: equal inputs
+ * give equal bits.  A logit of -inf (or of its type's lowest value beside larger ones) is an action
+ * of probability zero.  Rows that do not count (pl_rows) are not read: whatever their logits,
+ * actions or other entries hold, their outputs are zero.  A row that counts whose action is
+ * outside [0, n_actions) or has probability zero adds nothing to a loss or a gradient (its
+ * gradient is zero, its weight stays with the rows' number) and gets the log probability NaN
+ * respectively -inf (NaN too where every logit of the row is -inf).  NaN and +inf logits of a row that counts give NaN: in its outputs and in the loss.
+ *
+ * All arrays are device memory, calls are asynchronous on `stream`, allocate nothing and can be
+ * captured into a HIP graph.  `workspace` is device memory of at least the bytes that the matching
+ * _workspace function names, 16-byte aligned, for the duration of the call (a call
+ * leaves nothing in it that a later one reads); calls that overlap in time need one each. */
+enum { PL_F32 = 0, PL_BF16 = 1, PL_F16 = 2 };
+
+typedef struct {
+    const void *data;       /* dev, [n_rows, n_actions] of `dtype`, aligned to its elements        */
+    int64_t n_rows;         /* 0 .. 2^31 - 1                                                       */
+    int64_t row_stride;     /* elements from a row to the next, >= n_actions                       */
+    int32_t n_actions;      /* 1 .. 2^24                                                           */
+    int32_t dtype;          /* PL_F32, PL_BF16 or PL_F16                                           */
+} pl_logits;
+
+/* How rows belong to sequences (episodes, texts), and which rows count.  A NULL pl_rows * is one
+ * sequence of all rows.
+ *   PL_ROWS_BY_SEQ   row s * L + i is step i of sequence s, L = n_rows / n_seqs
+ *   PL_ROWS_BY_STEP  row i * n_seqs + s is step i of sequence s (what an episode over a batch records)
+ *   PL_ROWS_PACKED   row bounds[s] + i is step i of sequence s
+ *   bounds  dev int32.  The first two: [n_seqs] lengths, or NULL when every sequence has all L steps;
+ *           steps at or past a sequence's length do not count.  Packed: [n_seqs + 1] ascending offsets
+ *           (required); rows in front of the first and from the last on do not count.
+ *   mask    dev [n_rows]: 0 = the row does not count; NULL = all do */
+enum { PL_ROWS_BY_SEQ = 0, PL_ROWS_BY_STEP = 1, PL_ROWS_PACKED = 2 };
+typedef struct {
+    int32_t n_seqs;         /* >= 1 (n_rows a multiple of it unless packed)                        */
+    int32_t order;
+    const int32_t *bounds;
+    const uint8_t *mask;
+} pl_rows;
+
+/* Bytes of workspace that any of the three calls below needs for these sizes (rows may be NULL, n_pairs 0);
+ * 0 if a size is out of range. */
+size_t pl_loss_workspace(const pl_logits *logits, const pl_rows *rows, int32_t n_pairs);
+
+/* Log probabilities of given actions, log softmax(logits[n])[actions[n]], and the entropies
+ * of the rows' distributions: old and reference log probabilities of the losses below, or scores of tokens.
+ *   actions      dev [n_rows] int32
+ *   out_logp     dev [n_rows] fp32;  out_entropy  dev [n_rows] fp32 or NULL */
+int pl_action_logp(const pl_logits *logits, const int32_t *actions, float *out_logp, float *out_entropy,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* The clipped policy loss with a KL and an entropy term.  Per row, with l = log pi(a),
+ * r = exp(l - old), d = ref - l, H the entropy of the row's distribution:
+ *     value = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coeff (e^d - d - 1) - entropy_coeff H
+ * and the loss is the sum over the rows that count of w times the value.  e^d - d - 1 >= 0 is the
+ * estimate of KL(pi || ref) from samples of pi whose derivative is kl_coeff (1 - e^d).
+ *   reduction    PL_REDUCE_ROWS: w = 1 / rows that count; PL_REDUCE_SEQS: w = 1 / (sequences with such rows x
+ *                rows of the sequence that count); PL_REDUCE_SUM: w = 1.  Nothing counts: loss and gradient are 0
+ *   grad_scale   factor of every derivative below (1 for the plain gradient of the loss)
+ *   advantages   dev [n_rows] fp32, or [n_seqs] with advantage_per_seq
+ *   old_logp     dev [n_rows] fp32: of the policy that took the actions; NULL: this one (r = 1)
+ *   ref_logp     dev [n_rows] fp32: of the reference; NULL: no KL term
+ *   out_stats    dev [5] fp32: loss; sums of w times the clipped surrogate (with its sign in the loss), the
+ *                KL estimate, the entropy; the share w of rows whose ratio was clipped
+ *   out_grad     dev [n_rows, n_actions] of the logits' type, rows grad_stride elements apart: d loss / d logits.
+ *                May be the logits themselves (same stride); NULL to skip
+ *   out_logp, out_entropy  dev [n_rows] fp32 or NULL
+ *   out_coeff, out_entropy_coeff  dev [n_rows] fp32 or NULL: minus d loss / d l and minus d loss / d H,
+ *                the weights that pl_policy_gradient_ex and pl_episode_gradient take (they ascend) */
+enum { PL_REDUCE_ROWS = 0, PL_REDUCE_SEQS = 1, PL_REDUCE_SUM = 2 };
+typedef struct {
+    float clip_low, clip_high;  /* >= 0, clip_low <= 1; infinity in clip_high: no upper edge         */
+    float kl_coeff, entropy_coeff;
+    float grad_scale;
+    int32_t reduction;
+    int32_t advantage_per_seq;  /* 0 or 1                                                          */
+} pl_policy_loss_cfg;
+int pl_clipped_policy_loss(const pl_logits *logits, const pl_rows *rows, const pl_policy_loss_cfg *cfg,
+                           const int32_t *actions, const float *advantages, const float *old_logp,
+                           const float *ref_logp, float *out_stats, void *out_grad, int64_t grad_stride,
+                           float *out_logp, float *out_entropy, float *out_coeff, float *out_entropy_coeff,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* The preference loss of paired log ratios.  With s_q the sum (or the mean) over the rows of sequence q that
+ * count of l - ref, and for every pair (better, worse) the margin m = beta (s_better - s_worse):
+ *     loss = mean over pairs of  -(1 - label_smoothing) log sigma(m) - label_smoothing log sigma(-m)
+ * A sequence may be in any number of pairs; a sequence without rows that count has s = 0.
+ *   pairs        dev [n_pairs, 2] int32: (better, worse) sequence ids; a pair with an id out of range is
+ *                left out (its margin is NaN).  NULL: pairs (0, 1), (2, 3), ..., n_pairs = n_seqs / 2.
+ *                (Lists take n_seqs x n_pairs comparisons.)
+ *   ref_logp     dev [n_rows] fp32 or NULL (no reference: 0)
+ *   out_stats    dev [2] fp32: loss, share of the pairs with m > 0
+ *   out_grad, grad_stride, out_logp, out_coeff   as above (grad_scale too)
+ *   out_seq_logp dev [n_seqs] fp32 or NULL: sum (mean) of l over the sequence
+ *   out_margins  dev [n_pairs] fp32 or NULL */
+typedef struct {
+    float beta;                 /* >= 0                                                            */
+    float label_smoothing;      /* 0 .. 1                                                          */
+    float grad_scale;
+    int32_t average;            /* 0: sums over a sequence's rows; 1: means                         */
+} pl_preference_cfg;
+int pl_preference_loss(const pl_logits *logits, const pl_rows *rows, const pl_preference_cfg *cfg,
+                       const int32_t *actions, const float *ref_logp, int32_t n_pairs, const int32_t *pairs,
+                       float *out_stats, void *out_grad, int64_t grad_stride, float *out_logp,
+                       float *out_seq_logp, float *out_margins, float *out_coeff, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* ---- the 2-norm of all gradients of a model together, and clipping to it:
+ *     norm = sqrt(sum over tensors and elements of g^2),   clipped = g * (max_norm / norm) if norm > max_norm, else g
+ * The sum is taken in float64 (no gradient overflows it, and its order is fixed), the product in fp32, rounded
+ * once.  A norm that is NaN or infinite is reported and leaves the gradients as they are.
+ *   n_tensors    >= 0
+ *   grads        host [n_tensors] of dev pointers, aligned to their elements (NULL where numel is 0)
+ *   clipped      host [n_tensors] of dev pointers for the results, or NULL: in place.  An entry may equal the
+ *                gradient's; otherwise the two must not overlap
+ *   numel        host [n_tensors] int64 >= 0;  dtype  host [n_tensors]: PL_F32, PL_BF16 or PL_F16
+ *   max_norm     >= 0; infinity: the norm only (and copies where clipped differs)
+ *   out_norm     dev [1] fp32: the norm before clipping
+ * The host arrays are read before the call returns.  Workspace, stream and capture as above. */
+size_t pl_clip_gradients_workspace(int32_t n_tensors);
+int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clipped, const int64_t *numel,
+                      const int32_t *dtype, float max_norm, float *out_norm, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
 /* ---- per-stage timing, for benchmarks.  While enabled, forward and gradient calls bracket each
  * kernel stage with HIP events on the caller's stream (the BW stages are those of the reverse
  * pass: head, pooling, per-node layers at the final states, the dependent chain, projection,

@@ -5,10 +5,14 @@ Importing this package does not load the library; the first call does, and fails
 if it has not been built (`python -m paper_1906_08879_amd.build`).
 """
 from .binding import (  # noqa: F401
+    DecisionRows,
     GraphBatch,
     ModelCfg,
     PlacetoError,
     Weights,
+    action_logp,
+    clip_gradients,
+    clipped_policy_loss,
     embed_forward,
     embed_forward_static,
     embed_forward_static_bytes,
@@ -19,8 +23,10 @@ from .binding import (  # noqa: F401
     episode_step,
     library_path,
     load_library,
+    loss_workspace_bytes,
     node_classes,
     policy_gradient,
+    preference_loss,
     reinforce_coeff,
     simulate_reward,
     simulate_runtime,

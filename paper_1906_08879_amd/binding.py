@@ -17,6 +17,8 @@ _LIB_PATH = os.path.join(_HERE, "libplaceto.so")
 _lib = None
 
 PL_WEIGHTS = {"fp32": 0, "bf16": 1}
+ROWS = {"by_seq": 0, "by_step": 1, "packed": 2}
+REDUCE = {"rows": 0, "seqs": 1, "sum": 2}
 STAGES = ("project", "sweep", "pool", "head", "bw_head", "bw_pool", "bw_acts", "bw_chain", "bw_proj", "bw_wgrad")
 
 
@@ -28,6 +30,27 @@ class ModelCfg(ctypes.Structure):
     _fields_ = [("D", ctypes.c_int32), ("H", ctypes.c_int32), ("n_layers", ctypes.c_int32),
                 ("k_sweeps", ctypes.c_int32), ("group_by_device", ctypes.c_int32),
                 ("weight_dtype", ctypes.c_int32), ("single_set", ctypes.c_int32)]
+
+
+class LogitsView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_rows", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("n_actions", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RowsView(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("order", ctypes.c_int32), ("bounds", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p)]
+
+
+class PolicyLossCfg(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coeff", ctypes.c_float),
+                ("entropy_coeff", ctypes.c_float), ("grad_scale", ctypes.c_float), ("reduction", ctypes.c_int32),
+                ("advantage_per_seq", ctypes.c_int32)]
+
+
+class PreferenceCfg(ctypes.Structure):
+    _fields_ = [("beta", ctypes.c_float), ("label_smoothing", ctypes.c_float), ("grad_scale", ctypes.c_float),
+                ("average", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -83,6 +106,16 @@ def load_library(path: Optional[str] = None):
                                                  ctypes.c_float, ctypes.c_float, vp, vp, vp, vp, vp]),
         "pl_simulate_reward": (ctypes.c_int, [vp, ctypes.c_int32, vp, vp, ctypes.c_float, ctypes.c_float,
                                               ctypes.c_float, vp, vp, vp, vp, vp]),
+        "pl_loss_workspace": (ctypes.c_size_t, [ctypes.POINTER(LogitsView), ctypes.POINTER(RowsView), ctypes.c_int32]),
+        "pl_action_logp": (ctypes.c_int, [ctypes.POINTER(LogitsView), vp, vp, vp, vp, ctypes.c_size_t, vp]),
+        "pl_clipped_policy_loss": (ctypes.c_int, [ctypes.POINTER(LogitsView), ctypes.POINTER(RowsView),
+                                                  ctypes.POINTER(PolicyLossCfg), vp, vp, vp, vp, vp, vp, ctypes.c_int64,
+                                                  vp, vp, vp, vp, vp, ctypes.c_size_t, vp]),
+        "pl_preference_loss": (ctypes.c_int, [ctypes.POINTER(LogitsView), ctypes.POINTER(RowsView),
+                                              ctypes.POINTER(PreferenceCfg), vp, vp, ctypes.c_int32, vp, vp, vp,
+                                              ctypes.c_int64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]),
+        "pl_clip_gradients_workspace": (ctypes.c_size_t, [ctypes.c_int32]),
+        "pl_clip_gradients": (ctypes.c_int, [ctypes.c_int32, vp, vp, vp, vp, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]),
         "pl_profile_enable": (ctypes.c_int, [vp, ctypes.c_int32]),
         "pl_profile_read": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_double), i64p,
                                            ctypes.c_int32]),
@@ -423,3 +456,210 @@ def simulate_reward(g: GraphBatch, D: int, node_feats, placement, inv_bandwidth:
     else:
         _check(lib.pl_simulate_reward_ex(*head, int(per_child_transfers), *tail), "pl_simulate_reward_ex")
     return out_reward
+
+
+# --------------------------------------------------------------------------- losses on rows of logits
+def _dtype_code(dtype, name):
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if code is None:
+        raise PlacetoError(f"{name}: expected float32, bfloat16 or float16, got {dtype}")
+    return code
+
+
+def _row_stride(t, name):
+    """Elements between the rows of a tensor [..., n_actions] whose rows lie at one distance from each other."""
+    if t.dim() < 2:
+        raise PlacetoError(f"{name}: expected [..., n_actions], got {tuple(t.shape)}")
+    sizes, strides = t.shape[:-1], t.stride()[:-1]
+    if t.numel() == 0:
+        return max(1, t.shape[-1])
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise PlacetoError(f"{name}: the logits of a row must lie side by side")
+    step = rows = None
+    for n, d in zip(reversed(sizes), reversed(strides)):
+        if n == 1:
+            continue
+        if step is None:
+            step, rows = d, n
+        elif d != step * rows:
+            raise PlacetoError(f"{name}: rows must lie at one distance from each other, got strides {t.stride()}")
+        else:
+            rows *= n
+    if step is not None and step < t.shape[-1]:
+        raise PlacetoError(f"{name}: rows overlap, got strides {t.stride()}")
+    return t.shape[-1] if step is None else step
+
+
+def _logits_view(logits):
+    import torch
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise PlacetoError("logits must be a device tensor")
+    code, stride = _dtype_code(logits.dtype, "logits"), _row_stride(logits, "logits")
+    V = int(logits.shape[-1])
+    n = int(logits.numel() // V) if V else 0
+    return LogitsView(logits.data_ptr(), n, stride, V, code), n
+
+
+def _out_grad(out_grad, logits):
+    """(pointer, row stride) of the gradient of the logits."""
+    import torch
+    if out_grad is None:
+        return None, 0
+    if not isinstance(out_grad, torch.Tensor) or not out_grad.is_cuda:
+        raise PlacetoError("out_grad must be a device tensor")
+    if out_grad.dtype != logits.dtype or out_grad.shape != logits.shape:
+        raise PlacetoError(f"out_grad: expected {logits.dtype} {tuple(logits.shape)}, got {out_grad.dtype} {tuple(out_grad.shape)}")
+    return out_grad.data_ptr(), _row_stride(out_grad, "out_grad")
+
+
+def _workspace(given, n_bytes, device, stream):
+    """Device memory for one call: the caller's, or new memory that belongs to the stream the call runs on."""
+    import torch
+    if given is not None:
+        if not isinstance(given, torch.Tensor) or not given.is_cuda or not given.is_contiguous():
+            raise PlacetoError("workspace must be a contiguous device tensor")
+        return given, given.numel() * given.element_size()
+    if stream is None:
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device), n_bytes
+    with torch.cuda.stream(stream):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device), n_bytes
+
+
+class DecisionRows:
+    """pl_rows: how n_rows rows belong to n_seqs sequences, and which count.
+
+    order   "by_seq" [sequences, steps], "by_step" [steps, sequences] or "packed"
+    bounds  int32 device tensor: lengths [n_seqs] (or None: all steps); packed: offsets [n_seqs + 1]
+    mask    bool or uint8 device tensor [n_rows], 0 = the row does not count, or None
+    The object keeps the tensors alive."""
+
+    def __init__(self, n_rows: int, n_seqs: int = 1, order: str = "by_seq", bounds=None, mask=None):
+        import torch
+        if order not in ROWS:
+            raise PlacetoError(f"order must be one of {sorted(ROWS)}")
+        if mask is not None and isinstance(mask, torch.Tensor) and mask.dtype == torch.bool:
+            mask = mask.view(torch.uint8)
+        self.n_rows, self.n_seqs, self.bounds, self.mask = int(n_rows), int(n_seqs), bounds, mask
+        self.view = RowsView(self.n_seqs, ROWS[order],
+                             _dev_ptr(bounds, torch.int32, self.n_seqs + (order == "packed"), "bounds"),
+                             _dev_ptr(mask, torch.uint8, self.n_rows, "mask"))
+
+
+def _rows_ref(rows, n):
+    if rows is None:
+        return None
+    if rows.n_rows != n:
+        raise PlacetoError(f"rows describes {rows.n_rows} rows, the logits have {n}")
+    return ctypes.byref(rows.view)
+
+
+def loss_workspace_bytes(logits, rows: Optional[DecisionRows] = None, n_pairs: int = 0) -> int:
+    """pl_loss_workspace: bytes that the calls below need for logits of this shape."""
+    view, n = _logits_view(logits)
+    return int(load_library().pl_loss_workspace(ctypes.byref(view), _rows_ref(rows, n), int(n_pairs)))
+
+
+def action_logp(logits, actions, out_logp, out_entropy=None, workspace=None, stream=None):
+    """pl_action_logp on device tensors: log probabilities (and entropies) of given actions under logits
+    [..., n_actions], fp32, bf16 or fp16."""
+    import torch
+    lib = load_library()
+    view, n = _logits_view(logits)
+    ref = ctypes.byref(view)
+    ws, ws_bytes = _workspace(workspace, lib.pl_loss_workspace(ref, None, 0), logits.device, stream)
+    _check(lib.pl_action_logp(ref, _dev_ptr(actions, torch.int32, n, "actions"),
+                              _dev_ptr(out_logp, torch.float32, n, "out_logp"),
+                              _dev_ptr(out_entropy, torch.float32, n, "out_entropy"), ws.data_ptr(), ws_bytes,
+                              _stream_ptr(stream)), "pl_action_logp")
+    return out_logp
+
+
+def clipped_policy_loss(logits, actions, advantages, out_stats, rows: Optional[DecisionRows] = None, old_logp=None,
+                        ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2, kl_coeff: float = 0.0,
+                        entropy_coeff: float = 0.0, reduction: str = "rows", advantage_per_sequence: bool = False,
+                        grad_scale: float = 1.0, out_grad=None, out_logp=None, out_entropy=None, out_coeff=None,
+                        out_entropy_coeff=None, workspace=None, stream=None):
+    """pl_clipped_policy_loss on device tensors.  out_stats [5]: loss, clipped surrogate, KL estimate, entropy,
+    share of clipped rows; out_grad like logits (may be the logits): d loss / d logits; out_coeff and
+    out_entropy_coeff: the weights that episode_gradient and policy_gradient take."""
+    import torch
+    lib = load_library()
+    if reduction not in REDUCE:
+        raise PlacetoError(f"reduction must be one of {sorted(REDUCE)}")
+    view, n = _logits_view(logits)
+    ref, rows_ref = ctypes.byref(view), _rows_ref(rows, n)
+    grad, grad_stride = _out_grad(out_grad, logits)
+    n_adv = (rows.n_seqs if rows is not None else 1) if advantage_per_sequence else n
+    cfg = PolicyLossCfg(clip_low, clip_high, kl_coeff, entropy_coeff, grad_scale, REDUCE[reduction], int(advantage_per_sequence))
+    ws, ws_bytes = _workspace(workspace, lib.pl_loss_workspace(ref, rows_ref, 0), logits.device, stream)
+    f32 = torch.float32
+    _check(lib.pl_clipped_policy_loss(
+        ref, rows_ref, ctypes.byref(cfg), _dev_ptr(actions, torch.int32, n, "actions"),
+        _dev_ptr(advantages, f32, n_adv, "advantages"), _dev_ptr(old_logp, f32, n, "old_logp"),
+        _dev_ptr(ref_logp, f32, n, "ref_logp"), _dev_ptr(out_stats, f32, 5, "out_stats"), grad, grad_stride,
+        _dev_ptr(out_logp, f32, n, "out_logp"), _dev_ptr(out_entropy, f32, n, "out_entropy"),
+        _dev_ptr(out_coeff, f32, n, "out_coeff"), _dev_ptr(out_entropy_coeff, f32, n, "out_entropy_coeff"),
+        ws.data_ptr(), ws_bytes, _stream_ptr(stream)), "pl_clipped_policy_loss")
+    return out_stats
+
+
+def preference_loss(logits, actions, rows: DecisionRows, out_stats, pairs=None, ref_logp=None, beta: float = 0.1,
+                    label_smoothing: float = 0.0, average: bool = False, grad_scale: float = 1.0, out_grad=None,
+                    out_logp=None, out_seq_logp=None, out_margins=None, out_coeff=None, workspace=None, stream=None):
+    """pl_preference_loss on device tensors.  pairs int32 [n_pairs, 2] of (better, worse) sequences, None: (0, 1),
+    (2, 3), ...; out_stats [2]: loss, share of pairs in the right order; out_grad and out_coeff as in
+    clipped_policy_loss."""
+    import torch
+    lib = load_library()
+    view, n = _logits_view(logits)
+    ref, rows_ref = ctypes.byref(view), _rows_ref(rows, n)
+    grad, grad_stride = _out_grad(out_grad, logits)
+    n_seqs = rows.n_seqs if rows is not None else 1
+    n_pairs = n_seqs // 2 if pairs is None else int(pairs.shape[0])
+    if pairs is not None and (pairs.dim() != 2 or pairs.shape[1] != 2):
+        raise PlacetoError(f"pairs: expected [n_pairs, 2], got {tuple(pairs.shape)}")
+    if pairs is None and n_seqs % 2:
+        raise PlacetoError("without pairs the number of sequences must be even")
+    cfg = PreferenceCfg(beta, label_smoothing, grad_scale, int(average))
+    ws, ws_bytes = _workspace(workspace, lib.pl_loss_workspace(ref, rows_ref, n_pairs), logits.device, stream)
+    f32 = torch.float32
+    _check(lib.pl_preference_loss(
+        ref, rows_ref, ctypes.byref(cfg), _dev_ptr(actions, torch.int32, n, "actions"),
+        _dev_ptr(ref_logp, f32, n, "ref_logp"), n_pairs, _dev_ptr(pairs, torch.int32, 2 * n_pairs, "pairs"),
+        _dev_ptr(out_stats, f32, 2, "out_stats"), grad, grad_stride, _dev_ptr(out_logp, f32, n, "out_logp"),
+        _dev_ptr(out_seq_logp, f32, n_seqs, "out_seq_logp"), _dev_ptr(out_margins, f32, n_pairs, "out_margins"),
+        _dev_ptr(out_coeff, f32, n, "out_coeff"), ws.data_ptr(), ws_bytes, _stream_ptr(stream)), "pl_preference_loss")
+    return out_stats
+
+
+def clip_gradients(grads, max_norm: float, out_norm, out=None, workspace=None, stream=None):
+    """pl_clip_gradients on device tensors: the 2-norm of all gradients together into out_norm [1], and the
+    gradients clipped to max_norm, in place or into the tensors of `out`.  Tensors are fp32, bf16 or fp16 and
+    contiguous."""
+    import torch
+    lib = load_library()
+    grads = list(grads)
+    n = len(grads)
+    out = None if out is None else list(out)
+    if out is not None and len(out) != n:
+        raise PlacetoError(f"out has {len(out)} tensors, grads {n}")
+    numel = [g.numel() for g in grads]
+    codes = [_dtype_code(g.dtype, "grads") for g in grads]
+    src = []
+    for i, g in enumerate(grads):
+        if not g.is_cuda or not g.is_contiguous():
+            raise PlacetoError(f"grads[{i}] must be a contiguous device tensor")
+        src.append(g.data_ptr())
+    dst = None
+    if out is not None:
+        for i, (o, g) in enumerate(zip(out, grads)):
+            if not o.is_cuda or not o.is_contiguous() or o.dtype != g.dtype or o.numel() != g.numel():
+                raise PlacetoError(f"out[{i}] must be a contiguous device tensor like its gradient")
+        dst = (ctypes.c_void_p * max(1, n))(*[o.data_ptr() for o in out])
+    ws, ws_bytes = _workspace(workspace, lib.pl_clip_gradients_workspace(n), out_norm.device, stream)
+    _check(lib.pl_clip_gradients(
+        n, (ctypes.c_void_p * max(1, n))(*src), dst, (ctypes.c_int64 * max(1, n))(*numel),
+        (ctypes.c_int32 * max(1, n))(*codes), float(max_norm), _dev_ptr(out_norm, torch.float32, 1, "out_norm"),
+        ws.data_ptr(), ws_bytes, _stream_ptr(stream)), "pl_clip_gradients")
+    return out_norm

@@ -1,0 +1,126 @@
+// Elements of the types that losses and gradients come in, 16 bytes at a time.
+#pragma once
+#include <cmath>
+#include <cstdint>
+
+#include "internal.h"
+
+namespace pl {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+    static constexpr int N = 4;        // elements of 16 bytes
+    static __device__ void unpack(const uint4 &v, float (&f)[4])
+    {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+    static __device__ uint4 pack(const float (&f)[4])
+    {
+        return {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    }
+    static __device__ float load(const float *p) { return *p; }
+    static __device__ void store(float *p, float f) { *p = f; }
+};
+template <>
+struct Elem<__bf16> {
+    static constexpr int N = 8;
+    static __device__ void unpack(const uint4 &v, float (&f)[8])
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ uint4 pack(const float (&f)[8])
+    {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){f[2 * i], f[2 * i + 1]}, bf16x2));
+        return {w[0], w[1], w[2], w[3]};
+    }
+    static __device__ float load(const __bf16 *p) { return static_cast<float>(*p); }
+    static __device__ void store(__bf16 *p, float f) { *p = static_cast<__bf16>(f); }
+};
+template <>
+struct Elem<_Float16> {
+    static constexpr int N = 8;
+    static __device__ void unpack(const uint4 &v, float (&f)[8])
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const halfx2 h = __builtin_bit_cast(halfx2, w[i]);
+            f[2 * i] = static_cast<float>(h.x);
+            f[2 * i + 1] = static_cast<float>(h.y);
+        }
+    }
+    static __device__ uint4 pack(const float (&f)[8])
+    {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = __builtin_bit_cast(uint32_t, (halfx2){static_cast<_Float16>(f[2 * i]), static_cast<_Float16>(f[2 * i + 1])});
+        return {w[0], w[1], w[2], w[3]};
+    }
+    static __device__ float load(const _Float16 *p) { return static_cast<float>(*p); }
+    static __device__ void store(_Float16 *p, float f) { *p = static_cast<_Float16>(f); }
+};
+
+// A row as slots of 16 aligned bytes: slot i holds elements i N - shift .. of the row, the first and
+// the last slot may reach past its ends and are taken an element at a time.
+template <typename T>
+struct Row {
+    static constexpr int N = Elem<T>::N;
+    const T *p;
+    int V, shift, slots;
+    __device__ Row(const void *data, int64_t stride, int64_t row, int V) : p(static_cast<const T *>(data) + row * stride), V(V)
+    {
+        shift = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+        slots = (V + shift + N - 1) / N;
+    }
+    __device__ int first(int slot) const { return slot * N - shift; }
+    __device__ void load(int slot, float (&f)[N], float outside) const
+    {
+        const int e = first(slot);
+        if (e >= 0 && e + N <= V) {
+            Elem<T>::unpack(*reinterpret_cast<const uint4 *>(p + e), f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = (e + i >= 0 && e + i < V) ? Elem<T>::load(p + e + i) : outside;
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void store_slot(T *out, bool aligned, int e, int V, const float (&f)[Elem<T>::N])
+{
+    constexpr int N = Elem<T>::N;
+    if (aligned && e >= 0 && e + N <= V) {
+        *reinterpret_cast<uint4 *>(out + e) = Elem<T>::pack(f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (e + i >= 0 && e + i < V) Elem<T>::store(out + e + i, f[i]);
+    }
+}
+
+template <typename F>
+void by_type(int dtype, F &&f)
+{
+    if (dtype == PL_BF16) f(__bf16{});
+    else if (dtype == PL_F16) f(_Float16{});
+    else f(float{});
+}
+
+}  // namespace
+}  // namespace pl

@@ -1,0 +1,111 @@
+// Internal declarations of the losses on rows of logits and of gradient clipping (include/placeto.h):
+// what their entry points hand to the kernels.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "internal.h"
+
+namespace pl {
+
+constexpr int kMaxActions = 1 << 24;
+constexpr int kMaxSlices = 64;         // parts that a row is cut into where there are few rows
+constexpr int kRowsPerBlock = 256;     // rows of a workgroup of the per-row kernels
+constexpr int kMaxSeqParts = 64;       // parts that the rows of a sequence are cut into
+
+struct LogitsView {
+    const void *data = nullptr;
+    int64_t n = 0, stride = 0;
+    int V = 1, dtype = PL_F32;
+};
+
+// Which sequence a row belongs to, and whether it counts (pl_rows).
+struct RowsView {
+    const int32_t *bounds = nullptr;
+    const uint8_t *mask = nullptr;
+    int64_t n = 0;
+    int S = 1, L = 0, order = PL_ROWS_BY_SEQ;
+    bool all = true;                   // every row counts, known on the host
+};
+
+// Rows that count, and sequences with such rows.
+struct RowTotals {
+    int32_t rows, seqs;
+};
+
+// Maximum, sum of exp(z - max) and sum of exp(z - max) (z - max) over a slice of a row.
+struct RowPart {
+    float m, s, t;
+};
+
+// The gradient of a row: exp(z_j - m) (A + B (z_j - m)) + C [j = a]; all three zero: zeros.
+struct RowGrad {
+    float m, A, B, C;
+};
+
+struct PolicyArgs {
+    const int32_t *actions;
+    const float *advantages, *old_logp, *ref_logp;
+    float *out_logp, *out_entropy, *out_coeff, *out_entropy_coeff;
+    float clip_low, clip_high, kl_coeff, entropy_coeff, grad_scale;
+    int reduction, advantage_per_seq;
+};
+
+struct PrefArgs {
+    const int32_t *actions;
+    const float *ref_logp;
+    float *out_logp, *out_seq_logp, *out_margins, *out_coeff;
+    const int32_t *pairs;
+    float beta, smoothing, grad_scale;
+    int average, n_pairs;
+};
+
+// One call's workspace, carved by carve_loss_workspace.
+struct LossWorkspace {
+    RowPart *parts = nullptr;          // [n, slices]
+    RowGrad *grad = nullptr;           // [n]
+    float *logp = nullptr;             // [n]
+    double *seq_part = nullptr;        // [parts of a sequence, S, 2] sums of l, of l - ref
+    int32_t *seq_part_n = nullptr;     // [parts of a sequence, S] rows that count
+    double *seq_sum = nullptr;         // [S, 2]
+    int32_t *seq_n = nullptr;          // [S]
+    float *seq_coeff = nullptr;        // [S]
+    RowTotals *totals = nullptr;       // [1]
+    double *sums = nullptr;            // [workgroups, 4]
+    int slices = 1, seq_parts = 1;
+    size_t bytes = 0;
+};
+
+LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsView &rows);
+
+// csrc/kernels_losses.hip
+void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_logp, float *out_entropy,
+                        const LossWorkspace &ws, hipStream_t s);
+void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, float *out_stats, void *out_grad,
+                        int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
+void launch_preference_loss(const LogitsView &x, const RowsView &rows, const PrefArgs &a, float *out_stats, void *out_grad,
+                            int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
+
+// csrc/kernels_clip.hip: tensors of one launch, passed by value (a kernel's arguments end at 4 KiB)
+constexpr int kClipTensors = 128;
+constexpr int kClipBlocks = 1024;
+struct ClipTable {
+    const void *src[kClipTensors];
+    void *dst[kClipTensors];
+    int64_t numel[kClipTensors];
+    int32_t first[kClipTensors + 1];   // chunks in front of each tensor
+    uint8_t dtype[kClipTensors];
+    int32_t n;
+};
+constexpr int64_t kClipChunk = 16384;  // elements of a chunk
+
+int clip_blocks(const ClipTable &t);    // workgroups, and partial sums, of a launch
+struct ClipFactor {                    // m 2^e
+    float m;
+    int32_t e;
+};
+void launch_clip_sums(const ClipTable &t, double *sums, hipStream_t s);
+void launch_clip_norm(const double *sums, int n_sums, float max_norm, float *out_norm, ClipFactor *factor, hipStream_t s);
+void launch_clip_scale(const ClipTable &t, const ClipFactor *factor, hipStream_t s);
+
+}  // namespace pl
