@@ -89,16 +89,16 @@ struct Row {
         slots = (V + shift + N - 1) / N;
     }
     __device__ int first(int slot) const { return slot * N - shift; }
-    __device__ void load(int slot, float (&f)[N], float outside) const
+    __device__ uint4 load(int slot, float outside) const
     {
         const int e = first(slot);
-        if (e >= 0 && e + N <= V) {
-            Elem<T>::unpack(*reinterpret_cast<const uint4 *>(p + e), f);
-        } else {
+        if (e >= 0 && e + N <= V) return *reinterpret_cast<const uint4 *>(p + e);
+        float f[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = (e + i >= 0 && e + i < V) ? Elem<T>::load(p + e + i) : outside;
-        }
+        for (int i = 0; i < N; ++i) f[i] = (e + i >= 0 && e + i < V) ? Elem<T>::load(p + e + i) : outside;
+        return Elem<T>::pack(f);
     }
+    __device__ void load(int slot, float (&f)[N], float outside) const { Elem<T>::unpack(load(slot, outside), f); }
 };
 
 template <typename T>

@@ -17,6 +17,7 @@ namespace pl {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kAddsNothing = INFINITY;   // in place of the l of a row that adds nothing to its sequence
 constexpr float kLowest = -200.0f;     // e^-200 is 0 in fp32: z - m below it stands for -infinity, whose product with 0 is NaN
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -116,6 +117,12 @@ __device__ __forceinline__ Place place_of(const RowsView &r, int64_t n)
     return p;
 }
 
+// l of a row to more than fp32: the sums over a sequence, whose difference to another one's counts, see no rounding of l.
+__device__ __forceinline__ double exact_l(const Sums &a, float z_a)
+{
+    return (static_cast<double>(z_a) - a.m) - log(static_cast<double>(a.s));
+}
+
 __device__ __forceinline__ double wave_sum(double v)
 {
 #pragma unroll
@@ -169,24 +176,28 @@ template <typename T>
 __global__ __launch_bounds__(kRowsPerBlock) void k_finish_logp(LogitsView x, RowsView rows, const int32_t *__restrict__ actions,
                                                                const RowPart *__restrict__ parts, int slices,
                                                                float *__restrict__ out_logp, float *__restrict__ out_entropy,
-                                                               float *__restrict__ logp, RowGrad *__restrict__ grad)
+                                                               double *__restrict__ logp, RowGrad *__restrict__ grad)
 {
     const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + threadIdx.x;
     if (n >= x.n) return;
     float l = 0.0f, H = 0.0f;
+    double exact = kAddsNothing;
     RowGrad g{0.0f, 0.0f, 0.0f, 0.0f};
     if (place_of(rows, n).counts) {
         const Sums a = merged_parts(parts + n * slices, slices);
         const int act = actions[n];
         const bool ok = act >= 0 && act < x.V;
+        const float z_a = ok ? logit<T>(x, n, act) : 0.0f;
         float log_s;
-        finish_row(a, ok ? logit<T>(x, n, act) : 0.0f, ok, l, H, log_s);
+        finish_row(a, z_a, ok, l, H, log_s);
         g.m = a.m;
-        g.A = (ok && l != -INFINITY) ? 1.0f / a.s : 0.0f;   // 0: the row adds nothing
-        if (a.s == 0.0f) g.A = 0.0f;
+        if (ok && l != -INFINITY && a.s != 0.0f) {
+            g.A = 1.0f / a.s;
+            exact = exact_l(a, z_a);
+        }
     }
     if (out_logp) out_logp[n] = l;
-    if (logp) logp[n] = l;
+    if (logp) logp[n] = exact;
     if (out_entropy) out_entropy[n] = H;
     if (grad) grad[n] = g;
 }
@@ -273,6 +284,28 @@ __global__ __launch_bounds__(kRowsPerBlock) void k_finish_policy(LogitsView x, R
     if (tid < 4) sums[static_cast<size_t>(blockIdx.x) * 4 + tid] = wave[0][tid] + wave[1][tid] + wave[2][tid] + wave[3][tid];
 }
 
+__device__ __forceinline__ void policy_stats_out(const double (&v)[4], float kl_coeff, float entropy_coeff, float *out)
+{
+    out[0] = static_cast<float>(v[0] + kl_coeff * v[1] - entropy_coeff * v[2]);
+    for (int i = 0; i < 4; ++i) out[1 + i] = static_cast<float>(v[i]);
+}
+
+// exp(z - m) (A + B (z - m)) of a slot
+template <int N>
+__device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g)
+{
+    if (g.B == 0.0f) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] - g.m) * g.A;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float d = f[j] - g.m;
+            f[j] = exp_of(d) * (g.A + g.B * fmaxf(d, kLowest));
+        }
+    }
+}
+
 // ---- the loss from the workgroups' sums, in their order
 __global__ __launch_bounds__(256) void k_policy_stats(const double *__restrict__ sums, int blocks, float kl_coeff,
                                                       float entropy_coeff, float *__restrict__ out)
@@ -289,51 +322,79 @@ __global__ __launch_bounds__(256) void k_policy_stats(const double *__restrict__
     __syncthreads();
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) v[i] = wave[0][i] + wave[1][i] + wave[2][i] + wave[3][i];
-        out[0] = static_cast<float>(v[0] + kl_coeff * v[1] - entropy_coeff * v[2]);
-        for (int i = 0; i < 4; ++i) out[1 + i] = static_cast<float>(v[i]);
+        policy_stats_out(v, kl_coeff, entropy_coeff, out);
     }
 }
 
-// ---- the gradient of the logits, an element at a time
+// ---- the gradient of the logits, an element at a time, kGradSlots slots of a row to a wave.  For a preference a row takes
+// its sequence's d loss / d l (seq_coeff) first.
+constexpr int kGradSlots = 256;
+
+struct GradArgs {
+    LogitsView x;
+    const int32_t *actions;
+    const RowGrad *grad;
+    void *out;
+    int64_t out_stride;
+    int chunks;                        // waves to a row
+    RowsView rows;                     // with seq_coeff
+    const float *seq_coeff;
+    float *out_coeff;
+    float grad_scale;
+};
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_row_grad(LogitsView x, const int32_t *__restrict__ actions,
-                                                  const RowGrad *__restrict__ grad, T *out, int64_t out_stride)
+__global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
 {
     constexpr int N = Elem<T>::N;
-    const int64_t n = blockIdx.x;
-    const RowGrad g = grad[n];
-    const Row<T> row(x.data, x.stride, n, x.V);
-    T *o = out + n * out_stride;
-    const bool aligned = (reinterpret_cast<uintptr_t>(o) & 15) == (reinterpret_cast<uintptr_t>(row.p) & 15);
-    const bool none = g.A == 0.0f && g.B == 0.0f && g.C == 0.0f;
-    const int act = none ? -1 : actions[n];
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < row.slots; i += gridDim.y * 256) {
-        float f[N];
-        const int e = row.first(i);
-        if (none) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) f[k] = 0.0f;
-        } else {
-            row.load(i, f, -INFINITY);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float d = f[k] - g.m;
-                f[k] = exp_of(d) * (g.B == 0.0f ? g.A : g.A + g.B * fmaxf(d, kLowest)) + (e + k == act ? g.C : 0.0f);
-            }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    for (int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + wave; id < a.x.n * a.chunks; id += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t n = id / a.chunks;
+        const int chunk = static_cast<int>(id - n * a.chunks);
+        RowGrad g = a.grad[n];
+        if (a.seq_coeff) {
+            const Place at = place_of(a.rows, n);
+            const float c = at.counts && g.A != 0.0f ? a.grad_scale * a.seq_coeff[at.seq] : 0.0f;
+            g.A = c == 0.0f ? 0.0f : -c * g.A;
+            g.C = c;
+            if (a.out_coeff && chunk == 0 && lane == 0) a.out_coeff[n] = -c;
         }
-        store_slot(o, aligned, e, x.V, f);
+        if (!a.out) continue;
+        const Row<T> row(a.x.data, a.x.stride, n, a.x.V);
+        T *o = static_cast<T *>(a.out) + n * a.out_stride;
+        const bool aligned = (reinterpret_cast<uintptr_t>(o) & 15) == (reinterpret_cast<uintptr_t>(row.p) & 15);
+        const bool none = g.A == 0.0f && g.B == 0.0f && g.C == 0.0f;
+        const int act = none ? -1 : a.actions[n];
+#pragma unroll
+        for (int k = 0; k < kGradSlots; k += 64) {
+            const int i = chunk * kGradSlots + k + lane;
+            if (i >= row.slots) break;
+            float f[N];
+            const int e = row.first(i);
+            if (none) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = 0.0f;
+            } else {
+                row.load(i, f, -INFINITY);
+                grad_slot<N>(f, g);
+                if (act >= e && act < e + N) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) f[j] += e + j == act ? g.C : 0.0f;
+                }
+            }
+            store_slot(o, aligned, e, a.x.V, f);
+        }
     }
 }
 
 // ---- sequences: sums of l and l - ref over the rows that count, and their number (with logp == nullptr: the
-// number only), of part blockIdx.y of every sequence.  64 / lanes_s rows of a sequence side by side in a wave.
-__global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const float *__restrict__ logp, const float *__restrict__ ref,
-                                                  const RowGrad *__restrict__ grad, int lanes_s, double *__restrict__ part,
-                                                  int32_t *__restrict__ part_n)
+// number only), of part blockIdx.y of every sequence: lanes_s sequences and 256 / lanes_s of their rows side by side.
+__global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *__restrict__ logp, const float *__restrict__ ref,
+                                                  int lanes_s, double *__restrict__ part, int32_t *__restrict__ part_n)
 {
     __shared__ double sum[256][2];
     __shared__ int32_t cnt[256];
-    const int tid = threadIdx.x, ls = tid % lanes_s, ms = tid / lanes_s, rows_abreast = 256 / lanes_s;
+    const int tid = threadIdx.x, ls = tid & (lanes_s - 1), ms = tid / lanes_s, abreast = 256 / lanes_s;
     const int q = blockIdx.x * lanes_s + ls;
     double a = 0.0, b = 0.0;
     int c = 0;
@@ -348,48 +409,53 @@ __global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const float *__
             if (rows.order == PL_ROWS_BY_STEP) step = rows.S;
         }
         const int64_t per = (len + gridDim.y - 1) / gridDim.y, end = min(len, per * (blockIdx.y + 1));
-        for (int64_t i = per * blockIdx.y + ms; i < end; i += rows_abreast) {
+#pragma unroll 4
+        for (int64_t i = per * blockIdx.y + ms; i < end; i += abreast) {
             const int64_t n = first + i * step;
-            if (rows.mask && !rows.mask[n]) continue;
-            ++c;
+            const bool in = !rows.mask || rows.mask[n];
+            c += in;
             if (!logp) continue;
-            const float l = logp[n];
-            if (grad && grad[n].A == 0.0f) continue;     // (a NaN from NaN logits is not 0)
-            a += l;
-            b += ref ? static_cast<double>(l) - ref[n] : l;
+            const double l = logp[n];
+            const float r = ref ? ref[n] : 0.0f;
+            if (in && l != kAddsNothing) {
+                a += l;
+                b += l - r;
+            }
         }
     }
     sum[tid][0] = a;
     sum[tid][1] = b;
     cnt[tid] = c;
-    __syncthreads();
-    if (tid < lanes_s && q < rows.S) {
-        for (int i = 1; i < rows_abreast; ++i) {
-            a += sum[i * lanes_s + tid][0];
-            b += sum[i * lanes_s + tid][1];
-            c += cnt[i * lanes_s + tid];
+    for (int o = 128; o >= lanes_s; o >>= 1) {
+        __syncthreads();
+        if (tid < o) {
+            sum[tid][0] += sum[tid + o][0];
+            sum[tid][1] += sum[tid + o][1];
+            cnt[tid] += cnt[tid + o];
         }
+    }
+    if (tid < lanes_s && q < rows.S) {
         const size_t at = static_cast<size_t>(blockIdx.y) * rows.S + q;
         if (part) {
-            part[at * 2] = a;
-            part[at * 2 + 1] = b;
+            part[at * 2] = sum[tid][0];
+            part[at * 2 + 1] = sum[tid][1];
         }
-        part_n[at] = c;
+        part_n[at] = cnt[tid];
     }
 }
 
-// Sums of the parts of every sequence, and over all sequences (one workgroup).
+// Sums of the parts of every sequence, eight lanes to one, and over all sequences (one workgroup).
 __global__ __launch_bounds__(1024) void k_seq_totals(int S, int seq_parts, const double *__restrict__ part,
                                                      const int32_t *__restrict__ part_n, double *__restrict__ seq_sum,
                                                      int32_t *__restrict__ seq_n, RowTotals *__restrict__ totals)
 {
     __shared__ int32_t wave[16][2];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 7;
     int rows = 0, seqs = 0;
-    for (int q = tid; q < S; q += 1024) {
+    for (int q = tid >> 3; q < S; q += 128) {
         double a = 0.0, b = 0.0;
         int c = 0;
-        for (int i = 0; i < seq_parts; ++i) {
+        for (int i = lane; i < seq_parts; i += 8) {
             const size_t at = static_cast<size_t>(i) * S + q;
             if (part) {
                 a += part[at * 2];
@@ -397,13 +463,21 @@ __global__ __launch_bounds__(1024) void k_seq_totals(int S, int seq_parts, const
             }
             c += part_n[at];
         }
-        if (part) {
-            seq_sum[q * 2] = a;
-            seq_sum[q * 2 + 1] = b;
+#pragma unroll
+        for (int o = 4; o; o >>= 1) {
+            a += __shfl_xor(a, o);
+            b += __shfl_xor(b, o);
+            c += __shfl_xor(c, o);
         }
-        seq_n[q] = c;
-        rows += c;
-        seqs += c > 0;
+        if (lane == 0) {
+            if (part) {
+                seq_sum[q * 2] = a;
+                seq_sum[q * 2 + 1] = b;
+            }
+            seq_n[q] = c;
+            rows += c;
+            seqs += c > 0;
+        }
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) {
@@ -454,43 +528,47 @@ __device__ __forceinline__ float d_margin(float m, float eps)
 
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))) + (x != x ? x : 0.0f); }
 
-// A thread per sequence; every workgroup goes over all pairs, 256 at a time through LDS, and adds those of its sequences in
-// the pairs' order.  The first workgroup adds up the loss.
+// A thread per sequence.  With a list of pairs every workgroup goes over all of them, 256 at a time through LDS, and adds
+// those of its sequences in the pairs' order; without one a sequence is in one pair.  The first workgroup adds up the loss.
 __global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *__restrict__ seq_sum,
                                                const int32_t *__restrict__ seq_n, float *__restrict__ seq_coeff,
                                                float *__restrict__ out_stats)
 {
-    __shared__ int sa[256], sb[256];
-    __shared__ float sg[256];
+    __shared__ int4 tile[256];
     __shared__ double wave[4][3];
     const int tid = threadIdx.x, q = blockIdx.x * 256 + tid;
     double loss = 0.0, right = 0.0, valid = 0.0, coeff = 0.0;
-    for (int i0 = 0; i0 < p.n_pairs; i0 += 256) {
-        const int i = i0 + tid;
-        Pair pr{-1, -1, false};
-        float m = NAN, g = 0.0f;
-        if (i < p.n_pairs) {
-            pr = pair_at(p, S, i);
-            if (pr.ok) {
-                m = static_cast<float>(p.beta * (seq_ratio(p, seq_sum, seq_n, pr.a, 1) - seq_ratio(p, seq_sum, seq_n, pr.b, 1)));
-                g = d_margin(m, p.smoothing);
-                loss += (1.0f - p.smoothing) * softplus(-m) + p.smoothing * softplus(m);
-                right += m > 0.0f;
-                valid += 1.0;
+    auto margin = [&](const Pair &pr) {
+        return static_cast<float>(p.beta * (seq_ratio(p, seq_sum, seq_n, pr.a, 1) - seq_ratio(p, seq_sum, seq_n, pr.b, 1)));
+    };
+    if (p.pairs || blockIdx.x == 0)
+        for (int i0 = 0; i0 < p.n_pairs; i0 += 256) {
+            const int i = i0 + tid;
+            Pair pr{-1, -1, false};
+            float m = NAN, g = 0.0f;
+            if (i < p.n_pairs) {
+                pr = pair_at(p, S, i);
+                if (pr.ok) {
+                    m = margin(pr);
+                    g = d_margin(m, p.smoothing);
+                    loss += (1.0f - p.smoothing) * softplus(-m) + p.smoothing * softplus(m);
+                    right += m > 0.0f;
+                    valid += 1.0;
+                }
+                if (blockIdx.x == 0 && p.out_margins) p.out_margins[i] = m;
             }
-            if (blockIdx.x == 0 && p.out_margins) p.out_margins[i] = m;
+            if (!p.pairs) continue;
+            __syncthreads();
+            tile[tid] = {pr.ok ? pr.a : -1, pr.ok ? pr.b : -1, __float_as_int(g), 0};
+            __syncthreads();
+            const int n = min(256, p.n_pairs - i0);
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const int4 e = tile[k];
+                const float v = __int_as_float(e.z);
+                coeff += (e.x == q ? v : 0.0f) - (e.y == q ? v : 0.0f);
+            }
         }
-        __syncthreads();
-        sa[tid] = pr.ok ? pr.a : -1;
-        sb[tid] = pr.ok ? pr.b : -1;
-        sg[tid] = g;
-        __syncthreads();
-        const int n = min(256, p.n_pairs - i0);
-        for (int k = 0; k < n; ++k) {
-            if (sa[k] == q) coeff += sg[k];
-            if (sb[k] == q) coeff -= sg[k];
-        }
-    }
     loss = wave_sum(loss);
     right = wave_sum(right);
     valid = wave_sum(valid);
@@ -500,13 +578,17 @@ __global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *
         wave[tid >> 6][2] = valid;
     }
     __syncthreads();
-    valid = wave[0][2] + wave[1][2] + wave[2][2] + wave[3][2];
+    valid = p.pairs ? wave[0][2] + wave[1][2] + wave[2][2] + wave[3][2] : p.n_pairs;
     const double per = valid > 0.0 ? 1.0 / valid : 0.0;
     if (blockIdx.x == 0 && tid == 0) {
         out_stats[0] = static_cast<float>((wave[0][0] + wave[1][0] + wave[2][0] + wave[3][0]) * per);
         out_stats[1] = static_cast<float>((wave[0][1] + wave[1][1] + wave[2][1] + wave[3][1]) * per);
     }
     if (q < S) {
+        if (!p.pairs && (q >> 1) < p.n_pairs) {
+            const float g = d_margin(margin(Pair{q & ~1, q | 1, true}), p.smoothing);
+            coeff = (q & 1) ? -g : g;
+        }
         coeff *= per * p.beta;
         if (p.average && seq_n[q] > 0) coeff /= seq_n[q];
         seq_coeff[q] = static_cast<float>(coeff);
@@ -514,21 +596,329 @@ __global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *
     }
 }
 
-// Every row takes its sequence's d loss / d l.
-__global__ __launch_bounds__(kRowsPerBlock) void k_pref_rows(RowsView rows, PrefArgs p, const float *__restrict__ seq_coeff,
-                                                             RowGrad *__restrict__ grad)
+// What a kernel that takes whole rows does with them.
+enum RowPass { PASS_LOGP, PASS_POLICY, PASS_PREF_FORWARD, PASS_PREF_GRAD };
+
+struct RowArgs {
+    LogitsView x;
+    RowsView rows;
+    uint32_t magic;                    // e / V = high word of e * magic (narrow rows)
+    const int32_t *actions;
+    float *out_logp, *out_entropy;
+    PolicyArgs policy;                 // PASS_POLICY
+    const RowTotals *totals;
+    const int32_t *seq_n;
+    double *sums;
+    float *out_stats;
+    double *logp;                      // PASS_PREF_FORWARD
+    RowGrad *grad;
+    const float *seq_coeff;            // PASS_PREF_GRAD
+    float *out_coeff;
+    float grad_scale;
+    void *out_grad;                    // both gradients
+    int64_t grad_stride;
+};
+
+// What follows from a row's sums: outputs, the row's part of the loss (added to `acc`) and its gradient.  `first`: this
+// thread writes the row's outputs and keeps its part.
+template <int PASS>
+__device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, const Place &p, const Sums &a, int act, float z_a, bool first,
+                                               double *acc)
 {
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + threadIdx.x;
-    if (n >= rows.n) return;
-    RowGrad g = grad[n];
-    const Place at = place_of(rows, n);
-    float c = 0.0f;
-    if (at.counts && g.A != 0.0f) c = p.grad_scale * seq_coeff[at.seq];
-    g.A = c == 0.0f ? 0.0f : -c * g.A;
-    g.C = c;
-    grad[n] = g;
-    if (p.out_coeff) p.out_coeff[n] = -c;
+    float l = 0.0f, H = 0.0f, log_s = 0.0f;
+    bool live = false;
+    if (p.counts) {
+        const bool ok = act >= 0 && act < g.x.V;
+        finish_row(a, z_a, ok, l, H, log_s);
+        live = ok && l != -INFINITY && a.s != 0.0f;
+    }
+    RowGrad rg{a.m, 0.0f, 0.0f, 0.0f};
+    if (PASS == PASS_POLICY) {
+        PolicyRow r;
+        if (live) {
+            r = policy_row(g.policy, n, p.seq, l, H, row_weight(g.rows, g.policy.reduction, g.totals, g.seq_n, p.seq));
+            rg = grad_of(r, g.policy, a, H, log_s);
+        }
+        if (first) {
+            acc[0] += r.sur;
+            acc[1] += r.kl;
+            acc[2] += r.H;
+            acc[3] += r.cut;
+            if (g.policy.out_coeff) g.policy.out_coeff[n] = r.c * g.policy.grad_scale;
+            if (g.policy.out_entropy_coeff) g.policy.out_entropy_coeff[n] = r.g * g.policy.grad_scale;
+        }
+    }
+    if (PASS == PASS_PREF_GRAD) {
+        const float c = live ? g.grad_scale * g.seq_coeff[p.seq] : 0.0f;
+        rg.C = c;
+        rg.A = c == 0.0f ? 0.0f : -c / a.s;
+        if (first && g.out_coeff) g.out_coeff[n] = -c;
+    } else if (first) {
+        if (g.out_logp) g.out_logp[n] = l;
+        if (g.out_entropy) g.out_entropy[n] = H;
+    }
+    if (PASS == PASS_PREF_FORWARD && first) {
+        g.logp[n] = live ? exact_l(a, z_a) : kAddsNothing;
+        if (g.grad) g.grad[n] = {a.m, live ? 1.0f / a.s : 0.0f, 0.0f, 0.0f};
+    }
+    return rg;
 }
+
+// The workgroup's part of the loss: into `sums`, or the loss itself where nobody else has a part.  wave[i][.]: wave i's.
+__device__ __forceinline__ void finish_sums(const RowArgs &g, const double (*wave)[4], int waves)
+{
+    if (threadIdx.x >= 4) return;
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    if (gridDim.x == 1) {
+        if (threadIdx.x) return;
+        for (int w = 0; w < waves; ++w)
+            for (int i = 0; i < 4; ++i) v[i] += wave[w][i];
+        policy_stats_out(v, g.policy.ref_logp ? g.policy.kl_coeff : 0.0f, g.policy.entropy_coeff, g.out_stats);
+    } else {
+        for (int w = 0; w < waves; ++w) v[0] += wave[w][threadIdx.x];
+        g.sums[static_cast<size_t>(blockIdx.x) * 4 + threadIdx.x] = v[0];
+    }
+}
+
+// ---- narrow rows (up to kNarrow actions): a row per thread, 256 rows through LDS, everything in one pass.
+// The rows' elements go in and out in the order they lie in memory, whatever their number; rows are an odd number
+// of words apart in LDS, so that the lanes' walks along their rows meet 32 different banks.
+// One pass over the elements of rows [n0, n0 + count): f(row, column, element in memory), in 16-byte slots where the rows lie
+// behind one another.
+template <typename T, bool STORE>
+__device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, int64_t n0, int count, int V, uint32_t magic, int pitch,
+                                            float *tile)
+{
+    constexpr int N = Elem<T>::N;
+    const int tid = threadIdx.x;
+    auto row_at = [&](int e) { return V == 1 ? e : static_cast<int>(__umulhi(static_cast<uint32_t>(e), magic)); };
+    if (stride == V) {
+        T *base = static_cast<T *>(const_cast<void *>(data)) + n0 * V;
+        const int total = count * V;
+        const Row<T> all(base, 0, 0, total);
+        for (int i = tid; i < all.slots; i += 256) {
+            float f[N];
+            const int e = all.first(i);
+            if (!STORE) all.load(i, f, 0.0f);
+            int r = row_at(max(e, 0)), c = max(e, 0) - r * V;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                if (e + k >= 0 && e + k < total) {
+                    if (STORE) f[k] = tile[r * pitch + c];
+                    else tile[r * pitch + c] = f[k];
+                    if (++c == V) {
+                        c = 0;
+                        ++r;
+                    }
+                }
+            }
+            if (STORE) store_slot(base, true, e, total, f);
+        }
+    } else {
+        for (int i = tid; i < count * V; i += 256) {
+            const int r = row_at(i), c = i - r * V;
+            T *p = static_cast<T *>(const_cast<void *>(data)) + (n0 + r) * stride + c;
+            if (STORE) Elem<T>::store(p, tile[r * pitch + c]);
+            else tile[r * pitch + c] = Elem<T>::load(p);
+        }
+    }
+}
+
+template <typename T, int PASS>
+__global__ __launch_bounds__(256) void k_narrow(RowArgs g)
+{
+    extern __shared__ float tile[];
+    __shared__ double wave[4][4];
+    constexpr bool kGrad = PASS == PASS_POLICY || PASS == PASS_PREF_GRAD;
+    const int V = g.x.V, pitch = V | 1, tid = threadIdx.x;
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int64_t n0 = static_cast<int64_t>(blockIdx.x) * 256; n0 < g.x.n; n0 += static_cast<int64_t>(gridDim.x) * 256) {
+        const int count = static_cast<int>(min(int64_t{256}, g.x.n - n0));
+        narrow_tile<T, false>(g.x.data, g.x.stride, n0, count, V, g.magic, pitch, tile);
+        __syncthreads();
+        if (tid < count) {
+            const int64_t n = n0 + tid;
+            float *z = tile + tid * pitch;
+            Sums a;
+            const Place p = place_of(g.rows, n);
+            const int act = p.counts ? g.actions[n] : -1;
+            if (p.counts) {
+                for (int j = 0; j < V; ++j) a.m = fmaxf(a.m, z[j]);
+                const float from = a.m == -INFINITY ? 0.0f : a.m;
+                for (int j = 0; j < V; ++j) {
+                    const float d = z[j] - from, e = exp_of(d);
+                    a.s += e;
+                    a.t += e * fmaxf(d, kLowest);
+                }
+            }
+            const RowGrad rg = finish_pass<PASS>(g, n, p, a, act, act >= 0 && act < V ? z[act] : 0.0f, true, acc);
+            if (kGrad && g.out_grad) {
+                const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
+                for (int j = 0; j < V; ++j) {
+                    float f[1] = {z[j]};
+                    grad_slot<1>(f, rg);
+                    z[j] = none ? 0.0f : f[0] + (j == act ? rg.C : 0.0f);
+                }
+            }
+        }
+        __syncthreads();
+        if (kGrad && g.out_grad) {
+            narrow_tile<T, true>(g.out_grad, g.grad_stride, n0, count, V, g.magic, pitch, tile);
+            __syncthreads();
+        }
+    }
+    if (PASS == PASS_POLICY) {
+        for (int i = 0; i < 4; ++i) {
+            const double v = wave_sum(acc[i]);
+            if ((tid & 63) == 0) wave[tid >> 6][i] = v;
+        }
+        __syncthreads();
+        finish_sums(g, wave, 4);
+    }
+}
+
+// The slot stays in its four registers: without this the compiler keeps every unpacked value from one use to the next.
+__device__ __forceinline__ void keep_packed(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+
+// ---- wider rows that fit in the registers of LANES threads: read once, the maximum and the sums of every wave, those of
+// the row in its first wave, the gradient from the registers.  Bound by memory: a pass that reads the row again for its
+// gradient moves a half more.
+// A lane holds CH slots of 16 aligned bytes, LANES apart, and one of the up to 2 N - 2 elements in front of the first and
+// behind the last whole slot.  Loads are predicated, with one value or -infinity in place of the others, so that all of
+// them are on their way before the first is waited for.
+template <typename T, int LANES, int CH, int PASS>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_waves_per_eu(CH == 16 ? 4 : 6))) void k_rows(RowArgs g)
+{
+    constexpr int N = Elem<T>::N, ROWS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / 64;
+    constexpr bool kGrad = PASS == PASS_POLICY;
+    constexpr bool kEntropy = PASS == PASS_POLICY || PASS == PASS_LOGP;
+    __shared__ RowPart part[WAVES > 1 ? WAVES : 1];
+    __shared__ RowGrad shared_grad;
+    __shared__ double loss[ROWS][4];               // of the rows that these lanes have had
+    const int tid = threadIdx.x, lane = tid & (LANES - 1);
+    const int V = g.x.V;
+    const int mine = LANES < 64 ? tid / LANES : LANES == 64 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
+    if (PASS == PASS_POLICY && lane < 4) loss[mine][lane] = 0.0;
+    if (PASS == PASS_POLICY) __syncthreads();
+    for (int64_t n = static_cast<int64_t>(blockIdx.x) * ROWS + mine; n < g.x.n; n += static_cast<int64_t>(gridDim.x) * ROWS) {
+        const T *row = static_cast<const T *>(g.x.data) + n * g.x.stride;
+        const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+        const int head = shift ? N - shift : 0, whole = (V - head) / N, tail = head + whole * N;
+        const int edge = lane < head ? lane : lane >= N && tail + lane - N < V && lane < 2 * N ? tail + lane - N : -1;
+        const Place p = place_of(g.rows, n);
+        const int act = p.counts ? g.actions[n] : -1;
+        const bool acts = act >= 0 && act < V;
+        uint4 v[CH];
+        float z_edge = -INFINITY, z_a = 0.0f;
+        Sums a;
+        if (p.counts) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __bf16>::value ? 0xff80ff80u : 0xfc00fc00u;
+                v[k] = {none, none, none, none};
+                if (k * LANES + lane < whole) v[k] = *(reinterpret_cast<const uint4 *>(row + head) + k * LANES + lane);
+            }
+            if (edge >= 0) z_edge = Elem<T>::load(row + edge);
+            if (acts) z_a = Elem<T>::load(row + act);
+            a.m = z_edge;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                float f[N];
+                Elem<T>::unpack(v[k], f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) a.m = fmaxf(a.m, f[j]);
+                keep_packed(v[k]);
+            }
+#pragma unroll
+            for (int o = (LANES < 64 ? LANES : 64) / 2; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor(a.m, o));
+            const float from = a.m == -INFINITY ? 0.0f : a.m;
+            auto add_one = [&](float z) {
+                const float d = z - from, e = exp_of(d);
+                a.s += e;
+                if (kEntropy) a.t += e * fmaxf(d, kLowest);
+            };
+            add_one(z_edge);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                if (k * LANES < whole) {
+                    float f[N];
+                    Elem<T>::unpack(v[k], f);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) add_one(f[j]);
+                }
+                keep_packed(v[k]);
+            }
+#pragma unroll
+            for (int o = (LANES < 64 ? LANES : 64) / 2; o; o >>= 1) {
+                a.s += __shfl_xor(a.s, o);
+                if (kEntropy) a.t += __shfl_xor(a.t, o);
+            }
+        }
+        RowGrad rg;
+        if (WAVES > 1) {
+            if ((tid & 63) == 0) part[tid >> 6] = {a.m, a.s, a.t};
+            __syncthreads();
+            if (tid < 64) {
+                const RowPart of = part[lane < WAVES ? lane : 0];
+                a = lane < WAVES ? Sums{of.m, of.s, of.t} : Sums{};
+#pragma unroll
+                for (int o = WAVES / 2; o; o >>= 1) a = merge(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)});
+                rg = finish_pass<PASS>(g, n, p, a, act, z_a, tid == 0, loss[0]);
+                if (tid == 0) shared_grad = rg;
+            }
+            __syncthreads();
+            rg = shared_grad;
+        } else {
+            rg = finish_pass<PASS>(g, n, p, a, act, z_a, lane == 0, loss[mine]);
+        }
+        if (kGrad && g.out_grad) {
+            T *o = static_cast<T *>(g.out_grad) + n * g.grad_stride;
+            const bool aligned = (reinterpret_cast<uintptr_t>(o + head) & 15) == 0;
+            const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                keep_packed(v[k]);
+                if (k * LANES + lane < whole) {
+                    float f[N];
+                    if (none) {
+#pragma unroll
+                        for (int j = 0; j < N; ++j) f[j] = 0.0f;
+                    } else {
+                        Elem<T>::unpack(v[k], f);
+                        grad_slot<N>(f, rg);
+                    }
+                    if (aligned) {
+                        *(reinterpret_cast<uint4 *>(o + head) + k * LANES + lane) = Elem<T>::pack(f);
+                    } else {
+                        T *at = o + head + (k * LANES + lane) * N;
+#pragma unroll
+                        for (int j = 0; j < N; ++j) Elem<T>::store(at + j, f[j]);
+                    }
+                }
+            }
+            if (edge >= 0) {
+                float f[1] = {z_edge};
+                grad_slot<1>(f, rg);
+                Elem<T>::store(o + edge, none ? 0.0f : f[0]);
+            }
+            // the action's own logit: written once more by the lane that has written it
+            if (!none && acts) {
+                const int slot = (act - head) / N;
+                if (act >= head && act < tail ? lane == (slot & (LANES - 1)) : edge == act) {
+                    float f[1] = {z_a};
+                    grad_slot<1>(f, rg);
+                    Elem<T>::store(o + act, f[0] + rg.C);
+                }
+            }
+        }
+    }
+    if (PASS == PASS_POLICY) {
+        __syncthreads();
+        finish_sums(g, loss, ROWS);
+    }
+}
+
+bool few_rows(const LogitsView &x) { return x.n < 64 && x.V >= 16384; }
 
 int row_blocks(int64_t n) { return static_cast<int>((n + kRowsPerBlock - 1) / kRowsPerBlock); }
 
@@ -540,26 +930,84 @@ void launch_parts(const LogitsView &x, const RowsView &rows, const LossWorkspace
     });
 }
 
-void launch_grad(const LogitsView &x, const int32_t *actions, const LossWorkspace &ws, void *out, int64_t out_stride, hipStream_t s)
+void launch_grad(GradArgs a, hipStream_t s)
 {
-    by_type(x.dtype, [&](auto t) {
+    by_type(a.x.dtype, [&](auto t) {
         using T = decltype(t);
-        const int slots = x.V / Elem<T>::N + 2, per_block = 256 * 4;
-        hipLaunchKernelGGL(k_row_grad<T>, dim3(static_cast<uint32_t>(x.n), std::min((slots + per_block - 1) / per_block, 1024)),
-                           dim3(256), 0, s, x, actions, ws.grad, static_cast<T *>(out), out_stride);
+        a.chunks = a.out ? (a.x.V / Elem<T>::N + 2 + kGradSlots - 1) / kGradSlots : 1;
+        hipLaunchKernelGGL(k_row_grad<T>, dim3(static_cast<uint32_t>(std::min<int64_t>((a.x.n * a.chunks + 3) / 4, 1 << 22))), dim3(256), 0,
+                           s, a);
     });
 }
 
-void launch_seq_sums(const RowsView &rows, const float *logp, const float *ref, const LossWorkspace &ws, hipStream_t s)
+GradArgs grad_args(const LogitsView &x, const int32_t *actions, const LossWorkspace &ws, void *out, int64_t out_stride)
 {
-    // neighbouring rows of PL_ROWS_BY_STEP are of neighbouring sequences, of the other orders of one
-    int lanes_s = 1;
+    GradArgs a{};
+    a.x = x;
+    a.actions = actions;
+    a.grad = ws.grad;
+    a.out = out;
+    a.out_stride = out_stride;
+    return a;
+}
+
+// Sequences side by side in a workgroup of k_seq_sums: neighbouring rows of PL_ROWS_BY_STEP are of neighbouring
+// sequences, of the other orders of one.
+int seq_lanes(const RowsView &rows)
+{
+    int lanes = 1;
     if (rows.order == PL_ROWS_BY_STEP)
-        while (lanes_s < 64 && lanes_s < rows.S) lanes_s *= 2;
+        while (lanes < 64 && lanes < rows.S) lanes *= 2;
+    return lanes;
+}
+
+// Sums and numbers of rows of every sequence (logp), or their numbers and how many rows and sequences count in all.
+void launch_seq_sums(const RowsView &rows, const double *logp, const float *ref, const LossWorkspace &ws, hipStream_t s)
+{
+    const int lanes_s = seq_lanes(rows);
+    const bool whole = logp && ws.seq_parts == 1;
     hipLaunchKernelGGL(k_seq_sums, dim3((rows.S + lanes_s - 1) / lanes_s, ws.seq_parts), dim3(256), 0, s, rows, logp, ref,
-                       logp ? ws.grad : nullptr, lanes_s, logp ? ws.seq_part : nullptr, ws.seq_part_n);
-    hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows.S, ws.seq_parts, logp ? ws.seq_part : nullptr, ws.seq_part_n,
-                       ws.seq_sum, ws.seq_n, ws.totals);
+                       lanes_s, whole ? ws.seq_sum : logp ? ws.seq_part : nullptr, whole ? ws.seq_n : ws.seq_part_n);
+    if (!whole)
+        hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows.S, ws.seq_parts, logp ? ws.seq_part : nullptr, ws.seq_part_n,
+                           ws.seq_sum, ws.seq_n, ws.totals);
+}
+
+RowArgs row_args(const LogitsView &x, const RowsView &rows, const int32_t *actions)
+{
+    RowArgs g{};
+    g.x = x;
+    g.rows = rows;
+    g.actions = actions;
+    g.magic = x.V > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / x.V + 1) : 0;
+    return g;
+}
+
+// Whole rows in one pass (k_narrow, k_rows), and how many workgroups take them; 0 where they do not fit or where there are
+// so few of them that a row is better cut into slices.
+template <int PASS>
+int launch_rows(const RowArgs &g, hipStream_t s)
+{
+    int blocks = 0;
+    by_type(g.x.dtype, [&](auto t) {
+        using T = decltype(t);
+        const int slots = g.x.V / Elem<T>::N + 2;
+        auto go = [&](auto kernel, int rows, int threads, size_t lds, int most) {
+            blocks = static_cast<int>(std::min<int64_t>((g.x.n + rows - 1) / rows, most));
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, g);
+        };
+        if (g.x.V <= kNarrow) go(k_narrow<T, PASS>, 256, 256, 256 * (g.x.V | 1) * sizeof(float), kMaxSumBlocks);
+        if constexpr (PASS == PASS_PREF_GRAD) return;
+        else if (g.x.V <= kNarrow) return;
+        else if (slots <= 16 * 2) go(k_rows<T, 16, 2, PASS>, 16, 256, 0, kMaxSumBlocks);
+        else if (slots <= 64 * 4) go(k_rows<T, 64, 4, PASS>, 4, 256, 0, kMaxSumBlocks);
+        else if (slots <= 64 * 16) go(k_rows<T, 64, 16, PASS>, 4, 256, 0, kMaxSumBlocks);
+        else if (few_rows(g.x)) return;
+        else if (slots <= 256 * 16) go(k_rows<T, 256, 16, PASS>, 1, 256, 0, 1024);
+        else if (slots <= 512 * 16) go(k_rows<T, 512, 16, PASS>, 1, 512, 0, 512);
+        else if (slots <= 1024 * 16) go(k_rows<T, 1024, 16, PASS>, 1, 1024, 0, 256);
+    });
+    return blocks;
 }
 
 }  // namespace
@@ -575,10 +1023,12 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
     };
     const size_t n = static_cast<size_t>(x.n), S = static_cast<size_t>(rows.S);
     // a thousand workgroups where the rows are fewer, of 8192 logits at least
-    if (x.n > 0)
+    if (x.n > 0)    // (the workspace does not depend on which kernels run)
         w.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({1024 / x.n, x.V / 8192, kMaxSlices})));
-    const int64_t longest = rows.order == PL_ROWS_PACKED ? rows.n : rows.L;
-    w.seq_parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(longest / 2048, kMaxSeqParts)));
+    // sixteen rows to a thread of k_seq_sums, as long as the workgroups are few
+    const int64_t longest = rows.order == PL_ROWS_PACKED ? rows.n / rows.S : rows.L;
+    const int64_t per_part = 16 * (256 / seq_lanes(rows)), groups = (rows.S + seq_lanes(rows) - 1) / seq_lanes(rows);
+    w.seq_parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({(longest + per_part - 1) / per_part, kMaxSeqParts, 2048 / groups})));
     take(w.parts, n * w.slices);
     take(w.grad, n);
     take(w.logp, n);
@@ -588,7 +1038,7 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
     take(w.seq_n, S);
     take(w.seq_coeff, S);
     take(w.totals, 1);
-    take(w.sums, static_cast<size_t>(row_blocks(x.n)) * 4);
+    take(w.sums, static_cast<size_t>(std::max(row_blocks(x.n), kMaxSumBlocks)) * 4);
     w.bytes = pos;
     return w;
 }
@@ -599,6 +1049,10 @@ void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_
     RowsView rows;
     rows.n = x.n;
     rows.L = static_cast<int>(x.n);
+    RowArgs g = row_args(x, rows, actions);
+    g.out_logp = out_logp;
+    g.out_entropy = out_entropy;
+    if (launch_rows<PASS_LOGP>(g, s)) return;
     launch_parts(x, rows, ws, s);
     by_type(x.dtype, [&](auto t) {
         hipLaunchKernelGGL(k_finish_logp<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, actions, ws.parts,
@@ -609,24 +1063,46 @@ void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_
 void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, float *out_stats, void *out_grad,
                         int64_t grad_stride, const LossWorkspace &ws, hipStream_t s)
 {
+    if (x.n > 0 && !rows.all && a.reduction != PL_REDUCE_SUM) launch_seq_sums(rows, nullptr, nullptr, ws, s);
+    int blocks = row_blocks(x.n);
     if (x.n > 0) {
-        if (!rows.all && a.reduction != PL_REDUCE_SUM)
-            launch_seq_sums(rows, nullptr, nullptr, ws, s);
-        launch_parts(x, rows, ws, s);
-        by_type(x.dtype, [&](auto t) {
-            hipLaunchKernelGGL(k_finish_policy<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, a, ws.parts,
-                               ws.slices, ws.totals, ws.seq_n, out_grad ? ws.grad : nullptr, ws.sums);
-        });
+        RowArgs g = row_args(x, rows, a.actions);
+        g.policy = a;
+        g.out_logp = a.out_logp;
+        g.out_entropy = a.out_entropy;
+        g.totals = ws.totals;
+        g.seq_n = ws.seq_n;
+        g.sums = ws.sums;
+        g.out_stats = out_stats;
+        g.out_grad = out_grad;
+        g.grad_stride = grad_stride;
+        if (const int whole = launch_rows<PASS_POLICY>(g, s)) {
+            blocks = whole;
+            if (blocks == 1) return;             // the kernel has written the loss
+        } else {
+            launch_parts(x, rows, ws, s);
+            by_type(x.dtype, [&](auto t) {
+                hipLaunchKernelGGL(k_finish_policy<decltype(t)>, dim3(blocks), dim3(kRowsPerBlock), 0, s, x, rows, a, ws.parts,
+                                   ws.slices, ws.totals, ws.seq_n, out_grad ? ws.grad : nullptr, ws.sums);
+            });
+            if (out_grad) launch_grad(grad_args(x, a.actions, ws, out_grad, grad_stride), s);
+        }
     }
-    hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(256), 0, s, ws.sums, row_blocks(x.n), a.ref_logp ? a.kl_coeff : 0.0f,
+    hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(256), 0, s, ws.sums, blocks, a.ref_logp ? a.kl_coeff : 0.0f,
                        a.entropy_coeff, out_stats);
-    if (x.n > 0 && out_grad) launch_grad(x, a.actions, ws, out_grad, grad_stride, s);
 }
 
 void launch_preference_loss(const LogitsView &x, const RowsView &rows, const PrefArgs &a, float *out_stats, void *out_grad,
                             int64_t grad_stride, const LossWorkspace &ws, hipStream_t s)
 {
-    if (x.n > 0) {
+    RowArgs g = row_args(x, rows, a.actions);
+    g.out_logp = a.out_logp;
+    g.logp = ws.logp;
+    g.grad = ws.grad;
+    // rows that are read fast again whole need nothing kept of them
+    const bool again = x.V <= kNarrow;
+    if (again) g.grad = nullptr;
+    if (x.n > 0 && !launch_rows<PASS_PREF_FORWARD>(g, s)) {
         launch_parts(x, rows, ws, s);
         by_type(x.dtype, [&](auto t) {
             hipLaunchKernelGGL(k_finish_logp<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, a.actions,
@@ -635,9 +1111,21 @@ void launch_preference_loss(const LogitsView &x, const RowsView &rows, const Pre
     }
     launch_seq_sums(rows, ws.logp, a.ref_logp, ws, s);
     hipLaunchKernelGGL(k_pairs, dim3((rows.S + 255) / 256), dim3(256), 0, s, a, rows.S, ws.seq_sum, ws.seq_n, ws.seq_coeff, out_stats);
-    if (x.n > 0 && (out_grad || a.out_coeff)) {
-        hipLaunchKernelGGL(k_pref_rows, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, rows, a, ws.seq_coeff, ws.grad);
-        if (out_grad) launch_grad(x, a.actions, ws, out_grad, grad_stride, s);
+    if (x.n == 0 || (!out_grad && !a.out_coeff)) return;
+    if (again) {
+        g.out_coeff = a.out_coeff;
+        g.seq_coeff = ws.seq_coeff;
+        g.grad_scale = a.grad_scale;
+        g.out_grad = out_grad;
+        g.grad_stride = grad_stride;
+        launch_rows<PASS_PREF_GRAD>(g, s);
+    } else {
+        GradArgs ga = grad_args(x, a.actions, ws, out_grad, grad_stride);
+        ga.rows = rows;
+        ga.seq_coeff = ws.seq_coeff;
+        ga.out_coeff = a.out_coeff;
+        ga.grad_scale = a.grad_scale;
+        launch_grad(ga, s);
     }
 }
 

@@ -9,8 +9,10 @@
 namespace pl {
 
 constexpr int kMaxActions = 1 << 24;
+constexpr int kNarrow = 64;            // actions of rows that a thread takes
 constexpr int kMaxSlices = 64;         // parts that a row is cut into where there are few rows
 constexpr int kRowsPerBlock = 256;     // rows of a workgroup of the per-row kernels
+constexpr int kMaxSumBlocks = 2048;    // workgroups of the kernels that go over several rows
 constexpr int kMaxSeqParts = 64;       // parts that the rows of a sequence are cut into
 
 struct LogitsView {
@@ -38,7 +40,8 @@ struct RowPart {
     float m, s, t;
 };
 
-// The gradient of a row: exp(z_j - m) (A + B (z_j - m)) + C [j = a]; all three zero: zeros.
+// The gradient of a row: exp(z_j - m) (A + B (z_j - m)) + C [j = a]; all three zero: zeros.  Between the passes of a
+// preference, A is 1 / s (0: the row adds nothing).
 struct RowGrad {
     float m, A, B, C;
 };
@@ -64,14 +67,14 @@ struct PrefArgs {
 struct LossWorkspace {
     RowPart *parts = nullptr;          // [n, slices]
     RowGrad *grad = nullptr;           // [n]
-    float *logp = nullptr;             // [n]
+    double *logp = nullptr;            // [n]
     double *seq_part = nullptr;        // [parts of a sequence, S, 2] sums of l, of l - ref
     int32_t *seq_part_n = nullptr;     // [parts of a sequence, S] rows that count
     double *seq_sum = nullptr;         // [S, 2]
     int32_t *seq_n = nullptr;          // [S]
     float *seq_coeff = nullptr;        // [S]
     RowTotals *totals = nullptr;       // [1]
-    double *sums = nullptr;            // [workgroups, 4]
+    double *sums = nullptr;            // [workgroups, 4], at most kMaxSumBlocks or one per kRowsPerBlock rows
     int slices = 1, seq_parts = 1;
     size_t bytes = 0;
 };
