@@ -12,6 +12,14 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 
+typedef short shortx2 __attribute__((ext_vector_type(2)));
+
+// Two 16-bit elements of a word side by side.
+__device__ __forceinline__ uint32_t more_of_two(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(shortx2, a), __builtin_bit_cast(shortx2, b)));
+}
+
 template <typename T>
 struct Elem;
 template <>
@@ -25,6 +33,11 @@ struct Elem<float> {
     {
         return {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
     }
+    // The largest of values among which one is not negative has the largest bits as a signed number: a word's worth of
+    // elements with one integer instruction.
+    static constexpr uint32_t kLeast = 0x80000000u;
+    static __device__ uint32_t more(uint32_t a, uint32_t b) { return static_cast<uint32_t>(max(static_cast<int32_t>(a), static_cast<int32_t>(b))); }
+    static __device__ float largest(uint32_t a) { return __uint_as_float(a); }
     static __device__ float load(const float *p) { return *p; }
     static __device__ void store(float *p, float f) { *p = f; }
 };
@@ -47,6 +60,12 @@ struct Elem<__bf16> {
         for (int i = 0; i < 4; ++i)
             w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){f[2 * i], f[2 * i + 1]}, bf16x2));
         return {w[0], w[1], w[2], w[3]};
+    }
+    static constexpr uint32_t kLeast = 0x80008000u;
+    static __device__ uint32_t more(uint32_t a, uint32_t b) { return more_of_two(a, b); }
+    static __device__ float largest(uint32_t a)
+    {
+        return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
     }
     static __device__ float load(const __bf16 *p) { return static_cast<float>(*p); }
     static __device__ void store(__bf16 *p, float f) { *p = static_cast<__bf16>(f); }
@@ -71,6 +90,12 @@ struct Elem<_Float16> {
         for (int i = 0; i < 4; ++i)
             w[i] = __builtin_bit_cast(uint32_t, (halfx2){static_cast<_Float16>(f[2 * i]), static_cast<_Float16>(f[2 * i + 1])});
         return {w[0], w[1], w[2], w[3]};
+    }
+    static constexpr uint32_t kLeast = 0x80008000u;
+    static __device__ uint32_t more(uint32_t a, uint32_t b) { return more_of_two(a, b); }
+    static __device__ float largest(uint32_t a)
+    {
+        return fmaxf(static_cast<float>(__builtin_bit_cast(halfx2, a).x), static_cast<float>(__builtin_bit_cast(halfx2, a).y));
     }
     static __device__ float load(const _Float16 *p) { return static_cast<float>(*p); }
     static __device__ void store(_Float16 *p, float f) { *p = static_cast<_Float16>(f); }
@@ -101,12 +126,23 @@ struct Row {
     __device__ void load(int slot, float (&f)[N], float outside) const { Elem<T>::unpack(load(slot, outside), f); }
 };
 
+// 16 bytes to an address that is aligned to its elements only (one store instruction all the same, slower where a
+// cache line ends within it).
+typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
-__device__ __forceinline__ void store_slot(T *out, bool aligned, int e, int V, const float (&f)[Elem<T>::N])
+__device__ __forceinline__ void store_16(T *out, const uint4 &v)
+{
+    if (sizeof(T) == 4) *reinterpret_cast<words_at_4 *>(out) = words_at_4{v.x, v.y, v.z, v.w};
+    else *reinterpret_cast<words_at_2 *>(out) = words_at_2{v.x, v.y, v.z, v.w};
+}
+
+template <typename T>
+__device__ __forceinline__ void store_slot(T *out, int e, int V, const float (&f)[Elem<T>::N])
 {
     constexpr int N = Elem<T>::N;
-    if (aligned && e >= 0 && e + N <= V) {
-        *reinterpret_cast<uint4 *>(out + e) = Elem<T>::pack(f);
+    if (e >= 0 && e + N <= V) {
+        store_16(out + e, Elem<T>::pack(f));
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)

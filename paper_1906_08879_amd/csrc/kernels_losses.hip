@@ -1,12 +1,14 @@
 // Losses on rows of logits (include/placeto.h): log probabilities of actions, the clipped policy loss
 // and the preference loss, with the gradient of the logits.
 //
-// For a row z with maximum m:  s = sum_j e^{z_j - m},  t = sum_j e^{z_j - m} (z_j - m)  give
-//     l = log pi(a) = (z_a - m) - log s,      H = log s - t / s,
+// For a row z with maximum m, in powers of two: x_j = k z_j - o with k = log2 e and o = k m, rounded,
+// s = sum_j 2^{x_j} and t = sum_j 2^{x_j} x_j give
+//     l = log pi(a) = ln 2 (x_a - log2 s),      H = ln 2 (log2 s - t / s),
 // and with w c = d loss / d l and -w g = d loss / d H the gradient of logit j is
-//     w [ c (1[j = a] - p_j) + g p_j (log p_j + H) ] = e^{z_j - m} (A + B (z_j - m)) + C 1[j = a],
-//     C = w c,  B = w g / s,  A = (-w c + w g (H - log s)) / s.
-// z - m is taken before it is scaled, so rows of a type's lowest value, and rows far from zero, lose nothing.
+//     w [ c (1[j = a] - p_j) + g p_j (log p_j + H) ] = 2^{x_j} (A + B x_j) + C 1[j = a],
+//     C = w c,  B = ln 2 w g / s,  A = (-w c + w g (H - ln s)) / s.
+// x_j is one fused multiply-add, rounded once however far the row lies from zero: the rounding of o is the same for
+// every j and drops out of all three, that of k is a temperature of 1 + 2^-26.
 #include <algorithm>
 #include <cmath>
 
@@ -16,29 +18,98 @@
 namespace pl {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr double kAddsNothing = INFINITY;   // in place of the l of a row that adds nothing to its sequence
-constexpr float kLowest = -200.0f;     // e^-200 is 0 in fp32: z - m below it stands for -infinity, whose product with 0 is NaN
+constexpr float kLowest = -300.0f;     // 2^-300 is 0 in fp32: an x below it stands for -infinity, whose product with 0 is NaN
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+struct Ref {
+    float k, o;
+    __device__ float operator()(float z) const { return __builtin_fmaf(z, k, -o); }
+};
+
+// k and o of a maximum.  Past 2^126 logits are 2^103 apart or equal: with a smaller k, k m is an fp32 number, and
+// the differences are still far below any 2^x that is not 0.  A row of -infinity alone has sums of 0.
+__device__ __forceinline__ bool far_out(float m) { return fabsf(m) >= 0x1p126f; }
+__device__ __forceinline__ Ref ref_of(float m)
+{
+    if (m == -INFINITY) return {kLog2e, 0.0f};
+    const float k = far_out(m) ? 0x1p-20f : kLog2e;
+    return {k, m * k};
+}
+
+// ---- over 16 lanes (a DPP row) and over a wave
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
+__device__ __forceinline__ float max_of_16(float v)
+{
+    v = fmaxf(v, dpp<0x128>(v));       // rotations within the row by 8, 4, 2, 1
+    v = fmaxf(v, dpp<0x124>(v));
+    v = fmaxf(v, dpp<0x122>(v));
+    return fmaxf(v, dpp<0x121>(v));
+}
+
+__device__ __forceinline__ float sum_of_16(float v)
+{
+    v += dpp<0x128>(v);
+    v += dpp<0x124>(v);
+    v += dpp<0x122>(v);
+    return v + dpp<0x121>(v);
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+template <int LANES>
+__device__ __forceinline__ float max_of(float v)
+{
+    v = max_of_16(v);
+    if (LANES == 16) return v;
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
+template <int LANES>
+__device__ __forceinline__ float sum_of(float v)
+{
+    v = sum_of_16(v);
+    if (LANES == 16) return v;
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
 
 // ---- maximum and sums of a row
 struct Sums {
     float m = -INFINITY, s = 0.0f, t = 0.0f;
 };
 
-// The sums of both parts, relative to the larger maximum.  A part without a probability (s = 0) says nothing.
+// What a holds, relative to the maximum of b.  Sums without a probability (s = 0) say nothing.
+__device__ __forceinline__ Sums rebased(const Sums &a, float m, const Ref &to)
+{
+    if (a.s == 0.0f) return {m, 0.0f, 0.0f};
+    const float d = ref_of(a.m).o - to.o, e = exp2_of(d);
+    return {m, a.s * e, e * (a.t + fmaxf(d, kLowest) * a.s)};
+}
+
 __device__ __forceinline__ Sums merge(const Sums &a, const Sums &b)
 {
-    if (a.s == 0.0f) return b;
-    if (b.s == 0.0f) return a;
-    Sums r;
-    r.m = fmaxf(a.m, b.m);
-    const float da = fmaxf(a.m - r.m, kLowest), db = fmaxf(b.m - r.m, kLowest);
-    const float ea = exp_of(a.m - r.m), eb = exp_of(b.m - r.m);
-    r.s = a.s * ea + b.s * eb;
-    r.t = ea * (a.t + da * a.s) + eb * (b.t + db * b.s);
-    return r;
+    const float m = fmaxf(a.m, b.m);
+    const Ref to = ref_of(m);
+    const Sums x = rebased(a, m, to), y = rebased(b, m, to);
+    return {m, x.s + y.s, x.t + y.t};
+}
+
+template <int LANES>
+__device__ __forceinline__ Sums merge_of(const Sums &a)
+{
+    const float m = max_of<LANES>(a.m);
+    const Sums x = rebased(a, m, ref_of(m));
+    return {m, sum_of<LANES>(x.s), sum_of<LANES>(x.t)};
 }
 
 template <int N>
@@ -47,39 +118,14 @@ __device__ __forceinline__ void add(Sums &a, const float (&f)[N])
     float m = a.m;
 #pragma unroll
     for (int i = 0; i < N; ++i) m = fmaxf(m, f[i]);
-    if (m == -INFINITY) {                        // nothing but -infinity and NaN so far
-#pragma unroll
-        for (int i = 0; i < N; ++i) a.s += (f[i] != f[i]) ? f[i] : 0.0f;
-        return;
-    }
-    if (m != a.m) {
-        const float d = a.m - m;
-        if (a.s != 0.0f) {
-            const float e = exp_of(d);
-            a.t = e * (a.t + fmaxf(d, kLowest) * a.s);
-            a.s *= e;
-        }
-        a.m = m;
-    }
+    const Ref to = ref_of(m);
+    if (m != a.m) a = rebased(a, m, to);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float d = f[i] - m, e = exp_of(d);
+        const float x = to(f[i]), e = exp2_of(x);
         a.s += e;
-        a.t += e * fmaxf(d, kLowest);
+        a.t += e * fmaxf(x, kLowest);
     }
-}
-
-__device__ __forceinline__ Sums wave_merge(Sums a)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        Sums b;
-        b.m = __shfl_xor(a.m, o);
-        b.s = __shfl_xor(a.s, o);
-        b.t = __shfl_xor(a.t, o);
-        a = merge(a, b);
-    }
-    return a;
 }
 
 __device__ __forceinline__ Sums merged_parts(const RowPart *parts, int slices)
@@ -120,7 +166,9 @@ __device__ __forceinline__ Place place_of(const RowsView &r, int64_t n)
 // l of a row to more than fp32: the sums over a sequence, whose difference to another one's counts, see no rounding of l.
 __device__ __forceinline__ double exact_l(const Sums &a, float z_a)
 {
-    return (static_cast<double>(z_a) - a.m) - log(static_cast<double>(a.s));
+    const Ref ref = ref_of(a.m);
+    if (far_out(a.m)) return (static_cast<double>(z_a) - a.m) - log(static_cast<double>(a.s));
+    return 0.69314718055994530942 * ((static_cast<double>(z_a) * ref.k - ref.o) - log2(static_cast<double>(a.s)));
 }
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -130,12 +178,14 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
-// l and H of a row from its sums; a row without an allowed action has l = NaN, an action of probability zero l = -infinity.
+// l, H and log s of a row from its sums; a row without an allowed action has l = NaN, an action of probability zero
+// l = -infinity.
 __device__ __forceinline__ void finish_row(const Sums &a, float z_a, bool action_ok, float &l, float &H, float &log_s)
 {
-    log_s = logf(a.s);
-    H = log_s - a.t / a.s;
-    l = action_ok ? (z_a - a.m) - log_s : NAN;
+    const float log2_s = log2f(a.s);
+    log_s = kLn2 * log2_s;
+    H = kLn2 * (log2_s - a.t / a.s);
+    l = !action_ok ? NAN : far_out(a.m) ? (z_a - a.m) - log_s : kLn2 * (ref_of(a.m)(z_a) - log2_s);
     if (a.s == 0.0f) H = l = NAN;
 }
 
@@ -156,7 +206,7 @@ __global__ __launch_bounds__(256) void k_row_parts(LogitsView x, RowsView rows, 
         row.load(i, f, -INFINITY);
         add(a, f);
     }
-    a = wave_merge(a);
+    a = merge_of<64>(a);
     if ((tid & 63) == 0) wave[tid >> 6] = {a.m, a.s, a.t};
     __syncthreads();
     if (tid == 0) {
@@ -242,7 +292,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs &a, int64_t n, 
 __device__ __forceinline__ RowGrad grad_of(const PolicyRow &r, const PolicyArgs &a, const Sums &sums, float H, float log_s)
 {
     const float c = -r.c * a.grad_scale, g = r.g * a.grad_scale;
-    return {sums.m, (-c + g * (H - log_s)) / sums.s, g / sums.s, c};
+    return {sums.m, (-c + g * (H - log_s)) / sums.s, kLn2 * g / sums.s, c};
 }
 
 template <typename T>
@@ -290,18 +340,18 @@ __device__ __forceinline__ void policy_stats_out(const double (&v)[4], float kl_
     for (int i = 0; i < 4; ++i) out[1 + i] = static_cast<float>(v[i]);
 }
 
-// exp(z - m) (A + B (z - m)) of a slot
+// 2^x (A + B x) of a slot
 template <int N>
-__device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g)
+__device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g, const Ref &ref)
 {
     if (g.B == 0.0f) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] - g.m) * g.A;
+        for (int j = 0; j < N; ++j) f[j] = exp2_of(ref(f[j])) * g.A;
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const float d = f[j] - g.m;
-            f[j] = exp_of(d) * (g.A + g.B * fmaxf(d, kLowest));
+            const float x = ref(f[j]);
+            f[j] = exp2_of(x) * (g.A + g.B * fmaxf(x, kLowest));
         }
     }
 }
@@ -362,9 +412,9 @@ __global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
         if (!a.out) continue;
         const Row<T> row(a.x.data, a.x.stride, n, a.x.V);
         T *o = static_cast<T *>(a.out) + n * a.out_stride;
-        const bool aligned = (reinterpret_cast<uintptr_t>(o) & 15) == (reinterpret_cast<uintptr_t>(row.p) & 15);
         const bool none = g.A == 0.0f && g.B == 0.0f && g.C == 0.0f;
         const int act = none ? -1 : a.actions[n];
+        const Ref ref = ref_of(g.m);
 #pragma unroll
         for (int k = 0; k < kGradSlots; k += 64) {
             const int i = chunk * kGradSlots + k + lane;
@@ -376,13 +426,13 @@ __global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
                 for (int j = 0; j < N; ++j) f[j] = 0.0f;
             } else {
                 row.load(i, f, -INFINITY);
-                grad_slot<N>(f, g);
+                grad_slot<N>(f, g, ref);
                 if (act >= e && act < e + N) {
 #pragma unroll
                     for (int j = 0; j < N; ++j) f[j] += e + j == act ? g.C : 0.0f;
                 }
             }
-            store_slot(o, aligned, e, a.x.V, f);
+            store_slot(o, e, a.x.V, f);
         }
     }
 }
@@ -712,7 +762,7 @@ __device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, in
                     }
                 }
             }
-            if (STORE) store_slot(base, true, e, total, f);
+            if (STORE) store_slot(base, e, total, f);
         }
     } else {
         for (int i = tid; i < count * V; i += 256) {
@@ -744,19 +794,20 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
             const int act = p.counts ? g.actions[n] : -1;
             if (p.counts) {
                 for (int j = 0; j < V; ++j) a.m = fmaxf(a.m, z[j]);
-                const float from = a.m == -INFINITY ? 0.0f : a.m;
+                const Ref ref = ref_of(a.m);
                 for (int j = 0; j < V; ++j) {
-                    const float d = z[j] - from, e = exp_of(d);
+                    const float x = ref(z[j]), e = exp2_of(x);
                     a.s += e;
-                    a.t += e * fmaxf(d, kLowest);
+                    a.t += e * fmaxf(x, kLowest);
                 }
             }
             const RowGrad rg = finish_pass<PASS>(g, n, p, a, act, act >= 0 && act < V ? z[act] : 0.0f, true, acc);
             if (kGrad && g.out_grad) {
                 const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
+                const Ref ref = ref_of(rg.m);
                 for (int j = 0; j < V; ++j) {
                     float f[1] = {z[j]};
-                    grad_slot<1>(f, rg);
+                    grad_slot<1>(f, rg, ref);
                     z[j] = none ? 0.0f : f[0] + (j == act ? rg.C : 0.0f);
                 }
             }
@@ -791,16 +842,17 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
 {
     constexpr int N = Elem<T>::N, ROWS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / 64;
     constexpr bool kGrad = PASS == PASS_POLICY;
-    constexpr bool kEntropy = PASS == PASS_POLICY || PASS == PASS_LOGP;
     __shared__ RowPart part[WAVES > 1 ? WAVES : 1];
     __shared__ RowGrad shared_grad;
     __shared__ double loss[ROWS][4];               // of the rows that these lanes have had
-    const int tid = threadIdx.x, lane = tid & (LANES - 1);
+    const int tid = threadIdx.x;
+    int lane = tid & (LANES - 1);
     const int V = g.x.V;
     const int mine = LANES < 64 ? tid / LANES : LANES == 64 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
     if (PASS == PASS_POLICY && lane < 4) loss[mine][lane] = 0.0;
     if (PASS == PASS_POLICY) __syncthreads();
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * ROWS + mine; n < g.x.n; n += static_cast<int64_t>(gridDim.x) * ROWS) {
+        asm volatile("" : "+v"(lane));               // the slots' offsets are taken anew: kept over the rows they would cost CH registers
         const T *row = static_cast<const T *>(g.x.data) + n * g.x.stride;
         const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
         const int head = shift ? N - shift : 0, whole = (V - head) / N, tail = head + whole * N;
@@ -812,46 +864,57 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
         float z_edge = -INFINITY, z_a = 0.0f;
         Sums a;
         if (p.counts) {
+            const char *base = reinterpret_cast<const char *>(row + head);
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __bf16>::value ? 0xff80ff80u : 0xfc00fc00u;
-                v[k] = {none, none, none, none};
-                if (k * LANES + lane < whole) v[k] = *(reinterpret_cast<const uint4 *>(row + head) + k * LANES + lane);
-            }
+            for (int k = 0; k < CH; ++k)
+                if (k * LANES < whole)
+                    v[k] = *reinterpret_cast<const uint4 *>(base + static_cast<uint32_t>(min(k * LANES + lane, whole - 1)) * 16u);
             if (edge >= 0) z_edge = Elem<T>::load(row + edge);
             if (acts) z_a = Elem<T>::load(row + act);
-            a.m = z_edge;
+            constexpr int G = LANES < 64 ? LANES : 64;
+            uint32_t most[2] = {Elem<T>::kLeast, Elem<T>::kLeast};
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                float f[N];
-                Elem<T>::unpack(v[k], f);
-#pragma unroll
-                for (int j = 0; j < N; ++j) a.m = fmaxf(a.m, f[j]);
-                keep_packed(v[k]);
-            }
-#pragma unroll
-            for (int o = (LANES < 64 ? LANES : 64) / 2; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor(a.m, o));
-            const float from = a.m == -INFINITY ? 0.0f : a.m;
-            auto add_one = [&](float z) {
-                const float d = z - from, e = exp_of(d);
-                a.s += e;
-                if (kEntropy) a.t += e * fmaxf(d, kLowest);
-            };
-            add_one(z_edge);
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
+            for (int k = 0; k < CH; ++k)
                 if (k * LANES < whole) {
-                    float f[N];
-                    Elem<T>::unpack(v[k], f);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) add_one(f[j]);
+                    most[0] = Elem<T>::more(Elem<T>::more(most[0], v[k].x), v[k].y);
+                    most[1] = Elem<T>::more(Elem<T>::more(most[1], v[k].z), v[k].w);
                 }
-                keep_packed(v[k]);
-            }
+            // x is taken relative to the largest logit, or to 0 where all are negative: that is as good, unless they are far
+            // below
+            a.m = max_of<G>(fmaxf(z_edge, Elem<T>::largest(Elem<T>::more(most[0], most[1]))));
+            if (__float_as_int(a.m) < 0) a.m = 0.0f;
+            const Ref ref = ref_of(a.m);
+            auto add_all = [&](auto with_t) {
+                auto add_one = [&](float z) {
+                    const float x = ref(z), e = exp2_of(x);
+                    a.s += e;
+                    if (with_t) a.t += e * x;
+                };
+                if (edge >= 0) add_one(z_edge);
 #pragma unroll
-            for (int o = (LANES < 64 ? LANES : 64) / 2; o; o >>= 1) {
-                a.s += __shfl_xor(a.s, o);
-                if (kEntropy) a.t += __shfl_xor(a.t, o);
+                for (int k = 0; k < CH; ++k) {
+                    if (k * LANES + lane < whole) {
+                        float f[N];
+                        Elem<T>::unpack(v[k], f);
+#pragma unroll
+                        for (int j = 0; j < N; ++j) add_one(f[j]);
+                    }
+                    if (kGrad) keep_packed(v[k]);
+                }
+                a.s = sum_of<G>(a.s);
+                if (with_t) a.t = sum_of<G>(a.t);
+            };
+            if (PASS == PASS_POLICY || (PASS == PASS_LOGP && g.out_entropy)) add_all(std::true_type{});
+            else add_all(std::false_type{});
+            if (!(a.s >= 0x1p-100f) || a.t != a.t) {     // far below 0, -infinity among them, or not a number: once more, with care
+                a = Sums{};
+                const Row<T> again(g.x.data, g.x.stride, n, V);
+                for (int i = WAVES > 1 ? tid : lane; i < again.slots; i += LANES) {
+                    float f[N];
+                    again.load(i, f, -INFINITY);
+                    add(a, f);
+                }
+                a = merge_of<G>(a);
             }
         }
         RowGrad rg;
@@ -860,9 +923,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
             __syncthreads();
             if (tid < 64) {
                 const RowPart of = part[lane < WAVES ? lane : 0];
-                a = lane < WAVES ? Sums{of.m, of.s, of.t} : Sums{};
-#pragma unroll
-                for (int o = WAVES / 2; o; o >>= 1) a = merge(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)});
+                a = merge_of<64>(lane < WAVES ? Sums{of.m, of.s, of.t} : Sums{});
                 rg = finish_pass<PASS>(g, n, p, a, act, z_a, tid == 0, loss[0]);
                 if (tid == 0) shared_grad = rg;
             }
@@ -873,8 +934,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
         }
         if (kGrad && g.out_grad) {
             T *o = static_cast<T *>(g.out_grad) + n * g.grad_stride;
-            const bool aligned = (reinterpret_cast<uintptr_t>(o + head) & 15) == 0;
             const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
+            const Ref ref = ref_of(rg.m);
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 keep_packed(v[k]);
@@ -885,20 +946,14 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
                         for (int j = 0; j < N; ++j) f[j] = 0.0f;
                     } else {
                         Elem<T>::unpack(v[k], f);
-                        grad_slot<N>(f, rg);
+                        grad_slot<N>(f, rg, ref);
                     }
-                    if (aligned) {
-                        *(reinterpret_cast<uint4 *>(o + head) + k * LANES + lane) = Elem<T>::pack(f);
-                    } else {
-                        T *at = o + head + (k * LANES + lane) * N;
-#pragma unroll
-                        for (int j = 0; j < N; ++j) Elem<T>::store(at + j, f[j]);
-                    }
+                    store_16(o + head + static_cast<uint32_t>(k * LANES + lane) * N, Elem<T>::pack(f));
                 }
             }
             if (edge >= 0) {
                 float f[1] = {z_edge};
-                grad_slot<1>(f, rg);
+                grad_slot<1>(f, rg, ref);
                 Elem<T>::store(o + edge, none ? 0.0f : f[0]);
             }
             // the action's own logit: written once more by the lane that has written it
@@ -906,7 +961,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
                 const int slot = (act - head) / N;
                 if (act >= head && act < tail ? lane == (slot & (LANES - 1)) : edge == act) {
                     float f[1] = {z_a};
-                    grad_slot<1>(f, rg);
+                    grad_slot<1>(f, rg, ref);
                     Elem<T>::store(o + act, f[0] + rg.C);
                 }
             }

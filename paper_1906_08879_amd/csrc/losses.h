@@ -35,12 +35,12 @@ struct RowTotals {
     int32_t rows, seqs;
 };
 
-// Maximum, sum of exp(z - max) and sum of exp(z - max) (z - max) over a slice of a row.
+// Maximum m and sums over a slice of a row: of 2^x and of 2^x x, x = k z - o with k and o from m (ref_of).
 struct RowPart {
     float m, s, t;
 };
 
-// The gradient of a row: exp(z_j - m) (A + B (z_j - m)) + C [j = a]; all three zero: zeros.  Between the passes of a
+// The gradient of a row: 2^x (A + B x) + C [j = a], x = k z_j - o with k and o from m (ref_of); all three zero: zeros.  Between the passes of a
 // preference, A is 1 / s (0: the row adds nothing).
 struct RowGrad {
     float m, A, B, C;
