@@ -491,7 +491,7 @@ int pl_preference_loss(const pl_logits *logits, const pl_rows *rows, const pl_pr
  *   grads        host [n_tensors] of dev pointers, aligned to their elements (NULL where numel is 0)
  *   clipped      host [n_tensors] of dev pointers for the results, or NULL: in place.  An entry may equal the
  *                gradient's; otherwise the two must not overlap
- *   numel        host [n_tensors] int64 >= 0;  dtype  host [n_tensors]: PL_F32, PL_BF16 or PL_F16
+ *   numel        host [n_tensors] int64 >= 0, together at most 2^40;  dtype  host [n_tensors]: PL_F32, PL_BF16 or PL_F16
  *   max_norm     >= 0; infinity: the norm only (and copies where clipped differs)
  *   out_norm     dev [1] fp32: the norm before clipping
  * The host arrays are read before the call returns.  Workspace, stream and capture as above. */

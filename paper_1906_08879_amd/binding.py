@@ -151,13 +151,18 @@ def _dev_ptr(t, dtype, n_min, name):
     if t.dtype != dtype or not t.is_contiguous() or t.numel() < n_min:
         raise PlacetoError(f"{name}: expected contiguous {dtype} with >= {n_min} elements, "
                            f"got {t.dtype} {tuple(t.shape)}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream_ptr(stream):
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    # the current stream's handle without the Stream object around it, which costs as much as a kernel launch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device())
 
 
 def weights_count(D, H, n_layers=2, k_sweeps=1, group_by_device=1, weight_dtype="fp32") -> int:
@@ -459,45 +464,51 @@ def simulate_reward(g: GraphBatch, D: int, node_feats, placement, inv_bandwidth:
 
 
 # --------------------------------------------------------------------------- losses on rows of logits
+_DTYPE_CODES = {}
+
+
 def _dtype_code(dtype, name):
-    import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if not _DTYPE_CODES:
+        import torch
+        _DTYPE_CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    code = _DTYPE_CODES.get(dtype)
     if code is None:
         raise PlacetoError(f"{name}: expected float32, bfloat16 or float16, got {dtype}")
     return code
 
 
-def _row_stride(t, name):
+def _row_stride(t, shape, name):
     """Elements between the rows of a tensor [..., n_actions] whose rows lie at one distance from each other."""
-    if t.dim() < 2:
-        raise PlacetoError(f"{name}: expected [..., n_actions], got {tuple(t.shape)}")
-    sizes, strides = t.shape[:-1], t.stride()[:-1]
-    if t.numel() == 0:
-        return max(1, t.shape[-1])
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if len(shape) < 2:
+        raise PlacetoError(f"{name}: expected [..., n_actions], got {tuple(shape)}")
+    if t.is_contiguous():
+        return max(1, shape[-1])
+    strides = t.stride()
+    if shape[-1] > 1 and strides[-1] != 1:
         raise PlacetoError(f"{name}: the logits of a row must lie side by side")
     step = rows = None
-    for n, d in zip(reversed(sizes), reversed(strides)):
+    for n, d in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         if n == 1:
             continue
         if step is None:
             step, rows = d, n
         elif d != step * rows:
-            raise PlacetoError(f"{name}: rows must lie at one distance from each other, got strides {t.stride()}")
+            raise PlacetoError(f"{name}: rows must lie at one distance from each other, got strides {strides}")
         else:
             rows *= n
-    if step is not None and step < t.shape[-1]:
-        raise PlacetoError(f"{name}: rows overlap, got strides {t.stride()}")
-    return t.shape[-1] if step is None else step
+    if step is not None and step < shape[-1]:
+        raise PlacetoError(f"{name}: rows overlap, got strides {strides}")
+    return shape[-1] if step is None else step
 
 
 def _logits_view(logits):
     import torch
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
         raise PlacetoError("logits must be a device tensor")
-    code, stride = _dtype_code(logits.dtype, "logits"), _row_stride(logits, "logits")
-    V = int(logits.shape[-1])
-    n = int(logits.numel() // V) if V else 0
+    shape = logits.shape
+    code, stride = _dtype_code(logits.dtype, "logits"), _row_stride(logits, shape, "logits")
+    V = shape[-1]
+    n = logits.numel() // V if V else 0
     return LogitsView(logits.data_ptr(), n, stride, V, code), n
 
 
@@ -510,7 +521,7 @@ def _out_grad(out_grad, logits):
         raise PlacetoError("out_grad must be a device tensor")
     if out_grad.dtype != logits.dtype or out_grad.shape != logits.shape:
         raise PlacetoError(f"out_grad: expected {logits.dtype} {tuple(logits.shape)}, got {out_grad.dtype} {tuple(out_grad.shape)}")
-    return out_grad.data_ptr(), _row_stride(out_grad, "out_grad")
+    return out_grad.data_ptr(), _row_stride(out_grad, out_grad.shape, "out_grad")
 
 
 def _workspace(given, n_bytes, device, stream):
@@ -641,25 +652,22 @@ def clip_gradients(grads, max_norm: float, out_norm, out=None, workspace=None, s
     lib = load_library()
     grads = list(grads)
     n = len(grads)
-    out = None if out is None else list(out)
-    if out is not None and len(out) != n:
-        raise PlacetoError(f"out has {len(out)} tensors, grads {n}")
     numel = [g.numel() for g in grads]
-    codes = [_dtype_code(g.dtype, "grads") for g in grads]
-    src = []
-    for i, g in enumerate(grads):
-        if not g.is_cuda or not g.is_contiguous():
-            raise PlacetoError(f"grads[{i}] must be a contiguous device tensor")
-        src.append(g.data_ptr())
+    dtypes = [g.dtype for g in grads]
+    if not all([g.is_cuda and g.is_contiguous() for g in grads]):
+        raise PlacetoError("grads must be contiguous device tensors")
+    codes = {t: _dtype_code(t, "grads") for t in set(dtypes)}
     dst = None
     if out is not None:
-        for i, (o, g) in enumerate(zip(out, grads)):
-            if not o.is_cuda or not o.is_contiguous() or o.dtype != g.dtype or o.numel() != g.numel():
-                raise PlacetoError(f"out[{i}] must be a contiguous device tensor like its gradient")
-        dst = (ctypes.c_void_p * max(1, n))(*[o.data_ptr() for o in out])
+        out = list(out)
+        if len(out) != n:
+            raise PlacetoError(f"out has {len(out)} tensors, grads {n}")
+        if not all([o.is_cuda and o.is_contiguous() for o in out]) or [o.dtype for o in out] != dtypes or [o.numel() for o in out] != numel:
+            raise PlacetoError("out must be contiguous device tensors like their gradients")
+        dst = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out])
     ws, ws_bytes = _workspace(workspace, lib.pl_clip_gradients_workspace(n), out_norm.device, stream)
     _check(lib.pl_clip_gradients(
-        n, (ctypes.c_void_p * max(1, n))(*src), dst, (ctypes.c_int64 * max(1, n))(*numel),
-        (ctypes.c_int32 * max(1, n))(*codes), float(max_norm), _dev_ptr(out_norm, torch.float32, 1, "out_norm"),
+        n, (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]), dst, (ctypes.c_int64 * n)(*numel),
+        (ctypes.c_int32 * n)(*[codes[t] for t in dtypes]), float(max_norm), _dev_ptr(out_norm, torch.float32, 1, "out_norm"),
         ws.data_ptr(), ws_bytes, _stream_ptr(stream)), "pl_clip_gradients")
     return out_norm

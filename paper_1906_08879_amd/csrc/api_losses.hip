@@ -162,12 +162,12 @@ int pl_preference_loss(const pl_logits *logits, const pl_rows *rows_in, const pl
     return PL_OK;
 }
 
-// Sums of every launch's workgroups, and the factor behind them.
+// Sums of every launch's workgroups.
 size_t pl_clip_gradients_workspace(int32_t n_tensors)
 {
     if (n_tensors < 0) return 0;
     const size_t launches = (static_cast<size_t>(n_tensors) + kClipTensors - 1) / kClipTensors;
-    return (std::max<size_t>(1, launches) * kClipBlocks * sizeof(double)) + 16;
+    return std::max<size_t>(1, launches) * kClipBlocks * sizeof(double);
 }
 
 int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clipped, const int64_t *numel,
@@ -181,26 +181,32 @@ int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clippe
     if (!aligned_to(workspace, 16)) return fail(PL_ERR_SHAPE, "workspace must be aligned to 16 bytes");
     if (workspace_bytes < pl_clip_gradients_workspace(n_tensors))
         return fail(PL_ERR_SHAPE, "workspace holds fewer bytes than pl_clip_gradients_workspace names");
-    bool copies = max_norm < INFINITY;
+    bool scales = max_norm < INFINITY;           // whether anything is written but the norm
+    int64_t total = 0;
     for (int32_t i = 0; i < n_tensors; ++i) {
-        if (numel[i] < 0 || numel[i] > (int64_t{1} << 44)) return fail(PL_ERR_SHAPE, "numel must be 0 .. 2^44");
+        if (numel[i] < 0 || numel[i] > (int64_t{1} << 40) || total > (int64_t{1} << 40))
+            return fail(PL_ERR_SHAPE, "numel must not be negative, and all tensors together have at most 2^40 elements");
         if (!dtype_ok(dtype[i])) return fail(PL_ERR_SHAPE, "unknown type of a gradient");
+        total += numel[i];
         if (numel[i] == 0) continue;
         const size_t e = element_size(dtype[i]);
         if (!grads[i] || (clipped && !clipped[i])) return fail(PL_ERR_NULL, "a gradient or its result is NULL");
         if (!aligned_to(grads[i], e) || (clipped && !aligned_to(clipped[i], e)))
             return fail(PL_ERR_SHAPE, "gradients must be aligned to their elements");
-        copies = copies || (clipped && clipped[i] != grads[i]);
+        scales = scales || (clipped && clipped[i] != grads[i]);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     double *sums = static_cast<double *>(workspace);
     const size_t launches = (static_cast<size_t>(n_tensors) + kClipTensors - 1) / kClipTensors;
-    ClipFactor *factor = reinterpret_cast<ClipFactor *>(sums + std::max<size_t>(1, launches) * kClipBlocks);
-    // every launch's tensors, without the empty ones; the second pass takes the tables from the last to the first:
-    // what the first pass read last is the likeliest to be in the caches still
+    // every launch's tensors, without the empty ones; chunks as small as a workgroup's loads for a thread, as long as
+    // there are fewer of them than workgroups
+    // (a workgroup that does all alone takes a tensor at a time)
+    const bool small = n_tensors <= 4 && total <= kClipSmall;
+    const int chunk = small ? static_cast<int>(kClipSmall) : static_cast<int>(std::min<int64_t>(kClipChunk, std::max<int64_t>(2048, total / kClipBlocks / 2048 * 2048)));
     auto table = [&](size_t launch) {
         ClipTable t;
         t.n = 0;
+        t.chunk = chunk;
         t.first[0] = 0;
         const size_t end = std::min<size_t>(n_tensors, (launch + 1) * kClipTensors);
         for (size_t i = launch * kClipTensors; i < end; ++i) {
@@ -209,20 +215,30 @@ int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clippe
             t.dst[t.n] = clipped ? clipped[i] : grads[i];
             t.numel[t.n] = numel[i];
             t.dtype[t.n] = static_cast<uint8_t>(dtype[i]);
-            t.first[t.n + 1] = t.first[t.n] + static_cast<int32_t>((numel[i] + kClipChunk - 1) / kClipChunk);
+            t.first[t.n + 1] = t.first[t.n] + static_cast<int32_t>((numel[i] + chunk - 1) / chunk);
             ++t.n;
         }
         return t;
     };
-    int n_sums = 0;
-    for (size_t l = 0; l < launches; ++l) {
-        const ClipTable t = table(l);
-        launch_clip_sums(t, sums + n_sums, s);
-        n_sums += clip_blocks(t);
+    if (small) {
+        launch_clip_small(table(0), max_norm, out_norm, s);
+    } else {
+        int n_sums = 0;
+        for (size_t l = 0; l < launches; ++l) {
+            const ClipTable t = table(l);
+            launch_clip_sums(t, sums + n_sums, s);
+            n_sums += clip_blocks(t);
+        }
+        if (!scales) launch_clip_norm(sums, n_sums, out_norm, s);
+        bool first = true;                       // the norm is written by the first launch that has tensors
+        for (size_t l = launches; scales && l-- > 0;) {
+            const ClipTable t = table(l);
+            launch_clip_scale(t, sums, n_sums, max_norm, first ? out_norm : nullptr, s);
+            first = first && !clip_blocks(t);
+        }
+        // (tensors without elements alone: launches, but none of them has a workgroup)
+        if (scales && first) launch_clip_norm(sums, n_sums, out_norm, s);
     }
-    launch_clip_norm(sums, n_sums, max_norm, out_norm, factor, s);
-    if (copies)
-        for (size_t l = launches; l-- > 0;) launch_clip_scale(table(l), factor, s);
     PL_HIP(hipGetLastError());
     return PL_OK;
 }

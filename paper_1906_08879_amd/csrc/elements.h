@@ -126,6 +126,32 @@ struct Row {
     __device__ void load(int slot, float (&f)[N], float outside) const { Elem<T>::unpack(load(slot, outside), f); }
 };
 
+// The same elements as `whole` slots within the row and up to 2 N - 2 elements in front of and behind them, one of
+// which each of the first 2 N lanes can take (edge): loads of whole slots need no branch.
+template <typename T>
+struct Span {
+    static constexpr int N = Elem<T>::N;
+    const T *p;
+    int V, head, whole;
+    __device__ Span(const T *p, int V) : p(p), V(V)
+    {
+        const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+        head = shift ? min(N - shift, V) : 0;
+        whole = (V - head) / N;
+    }
+    __device__ int tail() const { return head + whole * N; }
+    __device__ int edge(int lane) const
+    {
+        if (lane < head) return lane;
+        return lane >= N && lane < 2 * N && tail() + lane - N < V ? tail() + lane - N : -1;
+    }
+    // (slot < whole; past it the last one again)
+    __device__ uint4 load(int slot) const
+    {
+        return *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p + head) + static_cast<uint32_t>(min(slot, whole - 1)) * 16u);
+    }
+};
+
 // 16 bytes to an address that is aligned to its elements only (one store instruction all the same, slower where a
 // cache line ends within it).
 typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));

@@ -1,9 +1,9 @@
 // The 2-norm of many gradients together, and clipping to it (include/placeto.h).
 //
-// Two passes over the gradients: squares summed in float64 (the square of any gradient fits, and
-// the conversions and fused multiply-adds of an element cost less than its bytes), then the product with
-// max_norm / norm.  The tensors come as a table by value, so that a call needs nothing on the device
-// that a captured graph or another stream could find changed.
+// Two passes over the gradients: the sum of squares, then the product with max_norm / norm; the second goes from the last
+// chunk to the first, so that what the first has read last is found in the caches.  Bound by memory (two reads and a
+// write).  The tensors come as a table by value, so that a call needs nothing on the device that a captured graph or
+// another stream could find changed.
 #include <algorithm>
 
 #include "elements.h"
@@ -13,12 +13,11 @@ namespace pl {
 namespace {
 
 struct Chunk {
-    int tensor;
+    int tensor, n;
     int64_t at;
-    int n;
 };
 
-// Chunk c of a table: the last tensor that begins at or in front of it.  (A tensor without elements has no chunk.)
+// Chunk c of a table: the last tensor that begins at or in front of it.  (A tensor without elements is not in the table.)
 __device__ __forceinline__ Chunk chunk_at(const ClipTable &t, int c)
 {
     int lo = 0, hi = t.n;
@@ -26,101 +25,172 @@ __device__ __forceinline__ Chunk chunk_at(const ClipTable &t, int c)
         const int mid = (lo + hi) >> 1;
         if (t.first[mid] <= c) lo = mid; else hi = mid;
     }
-    const int64_t at = static_cast<int64_t>(c - t.first[lo]) * kClipChunk;
-    return {lo, at, static_cast<int>(min(kClipChunk, t.numel[lo] - at))};
+    const int64_t at = static_cast<int64_t>(c - t.first[lo]) * t.chunk;
+    return {lo, static_cast<int>(min(static_cast<int64_t>(t.chunk), t.numel[lo] - at)), at};
 }
 
-template <typename T>
+// Squares of a slot: in fp32 where their sum is well within its range, which all but wild or vanished gradients are (one
+// conversion to a slot instead of one to an element, which took longer than the elements' bytes), else in float64.
+template <int N>
+__device__ __forceinline__ double slot_squares(const float (&f)[N])
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) s = __builtin_fmaf(f[k], f[k], s);
+    if (s > 0x1p-90f && s < 0x1p120f) return s;
+    double d = 0.0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) d = __builtin_fma(static_cast<double>(f[k]), static_cast<double>(f[k]), d);
+    return d;
+}
+
+// (kAhead loads of a thread are on their way together)
+constexpr int kAhead = 4;
+
+template <typename T, int THREADS>
 __device__ __forceinline__ double chunk_squares(const ClipTable &t, const Chunk &c)
 {
     constexpr int N = Elem<T>::N;
-    const Row<T> row(static_cast<const T *>(t.src[c.tensor]) + c.at, 0, 0, c.n);
+    const Span<T> span(static_cast<const T *>(t.src[c.tensor]) + c.at, c.n);
     double a = 0.0;
-    for (int i = threadIdx.x; i < row.slots; i += 256) {
-        float f[N];
-        row.load(i, f, 0.0f);
+    for (int i = threadIdx.x; i < span.whole; i += kAhead * THREADS) {
+        uint4 v[kAhead];
 #pragma unroll
-        for (int k = 0; k < N; ++k) a = __builtin_fma(static_cast<double>(f[k]), static_cast<double>(f[k]), a);
+        for (int k = 0; k < kAhead; ++k) v[k] = span.load(i + k * THREADS);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k * THREADS < span.whole) {
+                float f[N];
+                Elem<T>::unpack(v[k], f);
+                a += slot_squares<N>(f);
+            }
+    }
+    if (const int e = span.edge(threadIdx.x); e >= 0) {
+        const float f[1] = {Elem<T>::load(span.p + e)};
+        a += slot_squares<1>(f);
     }
     return a;
 }
 
-__device__ __forceinline__ double block_sum(double v)
+template <int THREADS>
+__device__ __forceinline__ double squares_of(const ClipTable &t, int chunk)
 {
-    __shared__ double wave[4];
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return wave[0] + wave[1] + wave[2] + wave[3];
+    const Chunk c = chunk_at(t, chunk);
+    const int dtype = t.dtype[c.tensor];
+    return dtype == PL_BF16 ? chunk_squares<__bf16, THREADS>(t, c)
+                            : dtype == PL_F16 ? chunk_squares<_Float16, THREADS>(t, c) : chunk_squares<float, THREADS>(t, c);
 }
 
-// max_norm / norm as mantissa and exponent: the quotient of a tiny limit and a huge norm is no fp32 number, its products are.
-__device__ __forceinline__ ClipFactor factor_of(double norm, float max_norm)
+// Sum over the workgroup, known to all of its threads.
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v)
 {
-    ClipFactor f{1.0f, 0};
-    if (norm > max_norm && norm < INFINITY) {
-        int e;
-        f.m = static_cast<float>(frexp(max_norm / norm, &e));
-        f.e = e;
-    }
+    __shared__ double wave[THREADS / 64];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) v += wave[i];
+    return v;
+}
+
+// max_norm / norm = m 2^e: the quotient of a tiny limit and a huge norm is no fp32 number, its products are.
+struct Factor {
+    float m;
+    int e;
+    __device__ bool is_one() const { return m == 1.0f && e == 0; }
+};
+
+__device__ __forceinline__ Factor factor_of(double norm, float max_norm)
+{
+    Factor f{1.0f, 0};
+    if (norm > max_norm && norm < INFINITY) f.m = static_cast<float>(frexp(max_norm / norm, &f.e));
     return f;
+}
+
+template <typename T, int THREADS>
+__device__ __forceinline__ void chunk_scale(const ClipTable &t, const Chunk &c, const Factor &by)
+{
+    constexpr int N = Span<T>::N;
+    const Span<T> span(static_cast<const T *>(t.src[c.tensor]) + c.at, c.n);
+    T *o = static_cast<T *>(t.dst[c.tensor]) + c.at;
+    if (by.is_one() && o == span.p) return;
+    for (int i = threadIdx.x; i < span.whole; i += kAhead * THREADS) {
+        uint4 v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) v[k] = span.load(i + k * THREADS);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k * THREADS < span.whole) {
+                if (!by.is_one()) {
+                    float f[N];
+                    Elem<T>::unpack(v[k], f);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) f[j] = ldexpf(f[j] * by.m, by.e);
+                    v[k] = Elem<T>::pack(f);
+                }
+                store_16(o + span.head + static_cast<uint32_t>(i + k * THREADS) * N, v[k]);
+            }
+    }
+    if (const int e = span.edge(threadIdx.x); e >= 0) {
+        const float f = Elem<T>::load(span.p + e);
+        Elem<T>::store(o + e, by.is_one() ? f : ldexpf(f * by.m, by.e));
+    }
+}
+
+template <int THREADS>
+__device__ __forceinline__ void scale_chunk(const ClipTable &t, int chunk, const Factor &by)
+{
+    const Chunk c = chunk_at(t, chunk);
+    const int dtype = t.dtype[c.tensor];
+    if (dtype == PL_BF16) chunk_scale<__bf16, THREADS>(t, c, by);
+    else if (dtype == PL_F16) chunk_scale<_Float16, THREADS>(t, c, by);
+    else chunk_scale<float, THREADS>(t, c, by);
 }
 
 __global__ __launch_bounds__(256) void k_clip_sums(ClipTable t, double *__restrict__ sums)
 {
     double a = 0.0;
-    for (int i = blockIdx.x; i < t.first[t.n]; i += gridDim.x) {
-        const Chunk c = chunk_at(t, i);
-        const int dtype = t.dtype[c.tensor];
-        a += dtype == PL_BF16 ? chunk_squares<__bf16>(t, c) : dtype == PL_F16 ? chunk_squares<_Float16>(t, c) : chunk_squares<float>(t, c);
-    }
-    a = block_sum(a);
+    for (int i = blockIdx.x; i < t.first[t.n]; i += gridDim.x) a += squares_of<256>(t, i);
+    a = block_sum<256>(a);
     if (threadIdx.x == 0) sums[blockIdx.x] = a;
 }
 
-__global__ __launch_bounds__(256) void k_clip_norm(const double *__restrict__ sums, int n, float max_norm, float *__restrict__ out_norm,
-                                                   ClipFactor *__restrict__ factor)
+// The norm from the workgroups' sums, in an order that depends on their number alone.
+__device__ __forceinline__ double norm_of(const double *__restrict__ sums, int n)
 {
     double a = 0.0;
     for (int i = threadIdx.x; i < n; i += 256) a += sums[i];
-    const double norm = sqrt(block_sum(a));
-    if (threadIdx.x == 0) {
-        *out_norm = static_cast<float>(norm);
-        *factor = factor_of(norm, max_norm);
-    }
+    return sqrt(block_sum<256>(a));
 }
 
-template <typename T>
-__device__ __forceinline__ void chunk_scale(const ClipTable &t, const Chunk &c, ClipFactor by)
+__global__ __launch_bounds__(256) void k_clip_norm(const double *__restrict__ sums, int n, float *__restrict__ out_norm)
 {
-    constexpr int N = Elem<T>::N;
-    const Row<T> row(static_cast<const T *>(t.src[c.tensor]) + c.at, 0, 0, c.n);
-    T *o = static_cast<T *>(t.dst[c.tensor]) + c.at;
-    const bool as_is = by.m == 1.0f && by.e == 0;
-    if (as_is && o == row.p) return;
-    for (int i = threadIdx.x; i < row.slots; i += 256) {
-        float f[N];
-        row.load(i, f, 0.0f);
-        if (!as_is) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) f[k] = ldexpf(f[k] * by.m, by.e);
-        }
-        store_slot(o, row.first(i), c.n, f);
-    }
+    const double norm = norm_of(sums, n);
+    if (threadIdx.x == 0) *out_norm = static_cast<float>(norm);
 }
 
-__global__ __launch_bounds__(256) void k_clip_scale(ClipTable t, const ClipFactor *__restrict__ factor)
+// Every workgroup takes the norm from the sums: 8 KiB out of the caches, instead of one more launch.
+__global__ __launch_bounds__(256) void k_clip_scale(ClipTable t, const double *__restrict__ sums, int n, float max_norm,
+                                                    float *__restrict__ out_norm)
 {
-    const ClipFactor f = *factor;
-    for (int i = blockIdx.x; i < t.first[t.n]; i += gridDim.x) {
-        const Chunk c = chunk_at(t, i);
-        const int dtype = t.dtype[c.tensor];
-        if (dtype == PL_BF16) chunk_scale<__bf16>(t, c, f);
-        else if (dtype == PL_F16) chunk_scale<_Float16>(t, c, f);
-        else chunk_scale<float>(t, c, f);
-    }
+    const double norm = norm_of(sums, n);
+    if (out_norm && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = static_cast<float>(norm);
+    const Factor by = factor_of(norm, max_norm);
+    for (int i = t.first[t.n] - 1 - blockIdx.x; i >= 0; i -= gridDim.x) scale_chunk<256>(t, i, by);
+}
+
+// Everything in one launch by one workgroup.
+__global__ __launch_bounds__(1024) void k_clip_small(ClipTable t, float max_norm, float *__restrict__ out_norm)
+{
+    double a = 0.0;
+    for (int i = 0; i < t.first[t.n]; ++i) a += squares_of<1024>(t, i);
+    const double norm = sqrt(block_sum<1024>(a));
+    if (threadIdx.x == 0) *out_norm = static_cast<float>(norm);
+    const Factor by = factor_of(norm, max_norm);
+    for (int i = t.first[t.n] - 1; i >= 0; --i) scale_chunk<1024>(t, i, by);
 }
 
 }  // namespace
@@ -132,14 +202,20 @@ void launch_clip_sums(const ClipTable &t, double *sums, hipStream_t s)
     if (clip_blocks(t)) hipLaunchKernelGGL(k_clip_sums, dim3(clip_blocks(t)), dim3(256), 0, s, t, sums);
 }
 
-void launch_clip_norm(const double *sums, int n_sums, float max_norm, float *out_norm, ClipFactor *factor, hipStream_t s)
+void launch_clip_norm(const double *sums, int n_sums, float *out_norm, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(256), 0, s, sums, n_sums, max_norm, out_norm, factor);
+    hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(256), 0, s, sums, n_sums, out_norm);
 }
 
-void launch_clip_scale(const ClipTable &t, const ClipFactor *factor, hipStream_t s)
+void launch_clip_scale(const ClipTable &t, const double *sums, int n_sums, float max_norm, float *out_norm, hipStream_t s)
 {
-    if (clip_blocks(t)) hipLaunchKernelGGL(k_clip_scale, dim3(clip_blocks(t)), dim3(256), 0, s, t, factor);
+    if (clip_blocks(t))
+        hipLaunchKernelGGL(k_clip_scale, dim3(clip_blocks(t)), dim3(256), 0, s, t, sums, n_sums, max_norm, out_norm);
+}
+
+void launch_clip_small(const ClipTable &t, float max_norm, float *out_norm, hipStream_t s)
+{
+    hipLaunchKernelGGL(k_clip_small, dim3(1), dim3(1024), 0, s, t, max_norm, out_norm);
 }
 
 }  // namespace pl

@@ -410,29 +410,42 @@ __global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
             if (a.out_coeff && chunk == 0 && lane == 0) a.out_coeff[n] = -c;
         }
         if (!a.out) continue;
-        const Row<T> row(a.x.data, a.x.stride, n, a.x.V);
+        const Span<T> row(static_cast<const T *>(a.x.data) + n * a.x.stride, a.x.V);
         T *o = static_cast<T *>(a.out) + n * a.out_stride;
         const bool none = g.A == 0.0f && g.B == 0.0f && g.C == 0.0f;
-        const int act = none ? -1 : a.actions[n];
+        const int act = none ? -1 : a.actions[n], edge = chunk == 0 ? row.edge(lane) : -1;
         const Ref ref = ref_of(g.m);
+        uint4 v[kGradSlots / 64];
+        float z_edge = 0.0f;
+        const int first = chunk * kGradSlots + lane;
+        if (!none) {
 #pragma unroll
-        for (int k = 0; k < kGradSlots; k += 64) {
-            const int i = chunk * kGradSlots + k + lane;
-            if (i >= row.slots) break;
-            float f[N];
-            const int e = row.first(i);
-            if (none) {
+            for (int k = 0; k < kGradSlots / 64; ++k) v[k] = row.load(first + k * 64);
+            if (edge >= 0) z_edge = Elem<T>::load(row.p + edge);
+        }
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = 0.0f;
-            } else {
-                row.load(i, f, -INFINITY);
-                grad_slot<N>(f, g, ref);
-                if (act >= e && act < e + N) {
+        for (int k = 0; k < kGradSlots / 64; ++k) {
+            const int slot = first + k * 64, e = row.head + slot * N;
+            if (slot < row.whole) {
+                float f[N];
+                if (none) {
 #pragma unroll
-                    for (int j = 0; j < N; ++j) f[j] += e + j == act ? g.C : 0.0f;
+                    for (int j = 0; j < N; ++j) f[j] = 0.0f;
+                } else {
+                    Elem<T>::unpack(v[k], f);
+                    grad_slot<N>(f, g, ref);
+                    if (act >= e && act < e + N) {
+#pragma unroll
+                        for (int j = 0; j < N; ++j) f[j] += e + j == act ? g.C : 0.0f;
+                    }
                 }
+                store_16(o + e, Elem<T>::pack(f));
             }
-            store_slot(o, e, a.x.V, f);
+        }
+        if (edge >= 0) {
+            float f[1] = {z_edge};
+            grad_slot<1>(f, g, ref);
+            Elem<T>::store(o + edge, none ? 0.0f : f[0] + (edge == act ? g.C : 0.0f));
         }
     }
 }
@@ -853,10 +866,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
     if (PASS == PASS_POLICY) __syncthreads();
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * ROWS + mine; n < g.x.n; n += static_cast<int64_t>(gridDim.x) * ROWS) {
         asm volatile("" : "+v"(lane));               // the slots' offsets are taken anew: kept over the rows they would cost CH registers
-        const T *row = static_cast<const T *>(g.x.data) + n * g.x.stride;
-        const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-        const int head = shift ? N - shift : 0, whole = (V - head) / N, tail = head + whole * N;
-        const int edge = lane < head ? lane : lane >= N && tail + lane - N < V && lane < 2 * N ? tail + lane - N : -1;
+        const Span<T> row(static_cast<const T *>(g.x.data) + n * g.x.stride, V);
+        const int head = row.head, whole = row.whole, edge = row.edge(lane);
         const Place p = place_of(g.rows, n);
         const int act = p.counts ? g.actions[n] : -1;
         const bool acts = act >= 0 && act < V;
@@ -864,13 +875,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
         float z_edge = -INFINITY, z_a = 0.0f;
         Sums a;
         if (p.counts) {
-            const char *base = reinterpret_cast<const char *>(row + head);
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (k * LANES < whole)
-                    v[k] = *reinterpret_cast<const uint4 *>(base + static_cast<uint32_t>(min(k * LANES + lane, whole - 1)) * 16u);
-            if (edge >= 0) z_edge = Elem<T>::load(row + edge);
-            if (acts) z_a = Elem<T>::load(row + act);
+                if (k * LANES < whole) v[k] = row.load(k * LANES + lane);
+            if (edge >= 0) z_edge = Elem<T>::load(row.p + edge);
+            if (acts) z_a = Elem<T>::load(row.p + act);
             constexpr int G = LANES < 64 ? LANES : 64;
             uint32_t most[2] = {Elem<T>::kLeast, Elem<T>::kLeast};
 #pragma unroll
@@ -959,7 +968,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
             // the action's own logit: written once more by the lane that has written it
             if (!none && acts) {
                 const int slot = (act - head) / N;
-                if (act >= head && act < tail ? lane == (slot & (LANES - 1)) : edge == act) {
+                if (act >= head && act < row.tail() ? lane == (slot & (LANES - 1)) : edge == act) {
                     float f[1] = {z_a};
                     grad_slot<1>(f, rg, ref);
                     Elem<T>::store(o + act, f[0] + rg.C);
@@ -989,7 +998,7 @@ void launch_grad(GradArgs a, hipStream_t s)
 {
     by_type(a.x.dtype, [&](auto t) {
         using T = decltype(t);
-        a.chunks = a.out ? (a.x.V / Elem<T>::N + 2 + kGradSlots - 1) / kGradSlots : 1;
+        a.chunks = a.out ? (a.x.V / Elem<T>::N + kGradSlots - 1) / kGradSlots : 1;
         hipLaunchKernelGGL(k_row_grad<T>, dim3(static_cast<uint32_t>(std::min<int64_t>((a.x.n * a.chunks + 3) / 4, 1 << 22))), dim3(256), 0,
                            s, a);
     });
@@ -1046,7 +1055,7 @@ int launch_rows(const RowArgs &g, hipStream_t s)
     int blocks = 0;
     by_type(g.x.dtype, [&](auto t) {
         using T = decltype(t);
-        const int slots = g.x.V / Elem<T>::N + 2;
+        const int slots = g.x.V / Elem<T>::N;    // whole ones, at most
         auto go = [&](auto kernel, int rows, int threads, size_t lds, int most) {
             blocks = static_cast<int>(std::min<int64_t>((g.x.n + rows - 1) / rows, most));
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, g);

@@ -98,17 +98,16 @@ struct ClipTable {
     int64_t numel[kClipTensors];
     int32_t first[kClipTensors + 1];   // chunks in front of each tensor
     uint8_t dtype[kClipTensors];
-    int32_t n;
+    int32_t n, chunk;                  // tensors; elements of a chunk
 };
-constexpr int64_t kClipChunk = 16384;  // elements of a chunk
+constexpr int kClipChunk = 16384;      // the most elements of a chunk
+constexpr int64_t kClipSmall = 32768;  // elements of a call that one workgroup does alone
 
-int clip_blocks(const ClipTable &t);    // workgroups, and partial sums, of a launch
-struct ClipFactor {                    // m 2^e
-    float m;
-    int32_t e;
-};
+int clip_blocks(const ClipTable &t);   // workgroups, and partial sums, of a launch
 void launch_clip_sums(const ClipTable &t, double *sums, hipStream_t s);
-void launch_clip_norm(const double *sums, int n_sums, float max_norm, float *out_norm, ClipFactor *factor, hipStream_t s);
-void launch_clip_scale(const ClipTable &t, const ClipFactor *factor, hipStream_t s);
+void launch_clip_norm(const double *sums, int n_sums, float *out_norm, hipStream_t s);
+// (writes out_norm, if given, as well)
+void launch_clip_scale(const ClipTable &t, const double *sums, int n_sums, float max_norm, float *out_norm, hipStream_t s);
+void launch_clip_small(const ClipTable &t, float max_norm, float *out_norm, hipStream_t s);
 
 }  // namespace pl
