@@ -159,8 +159,8 @@ typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
 __device__ __forceinline__ void store_16(T *out, const uint4 &v)
 {
-    if (sizeof(T) == 4) *reinterpret_cast<words_at_4 *>(out) = words_at_4{v.x, v.y, v.z, v.w};
-    else *reinterpret_cast<words_at_2 *>(out) = words_at_2{v.x, v.y, v.z, v.w};
+    if (sizeof(T) == 4) __builtin_nontemporal_store(words_at_4{v.x, v.y, v.z, v.w}, reinterpret_cast<words_at_4 *>(out));
+    else __builtin_nontemporal_store(words_at_2{v.x, v.y, v.z, v.w}, reinterpret_cast<words_at_2 *>(out));
 }
 
 template <typename T>

@@ -398,7 +398,9 @@ __global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
 {
     constexpr int N = Elem<T>::N;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    for (int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + wave; id < a.x.n * a.chunks; id += static_cast<int64_t>(gridDim.x) * 4) {
+    const int64_t ids = a.x.n * a.chunks;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + wave; i < ids; i += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t id = ids - 1 - i;              // from the last row to the first: what the pass before has read last first
         const int64_t n = id / a.chunks;
         const int chunk = static_cast<int>(id - n * a.chunks);
         RowGrad g = a.grad[n];
