@@ -189,32 +189,6 @@ __device__ __forceinline__ void finish_row(const Sums &a, float z_a, bool action
     if (a.s == 0.0f) H = l = NAN;
 }
 
-// ---- one slice of a row per workgroup: its maximum and sums
-template <typename T>
-__global__ __launch_bounds__(256) void k_row_parts(LogitsView x, RowsView rows, RowPart *__restrict__ parts, int slices)
-{
-    const int64_t n = blockIdx.x;
-    const int tid = threadIdx.x;
-    __shared__ RowPart wave[4];
-    if (!place_of(rows, n).counts) return;
-    const Row<T> row(x.data, x.stride, n, x.V);
-    const int per = (row.slots + slices - 1) / slices;
-    const int end = min(row.slots, per * (static_cast<int>(blockIdx.y) + 1));
-    Sums a;
-    for (int i = per * blockIdx.y + tid; i < end; i += 256) {
-        float f[Elem<T>::N];
-        row.load(i, f, -INFINITY);
-        add(a, f);
-    }
-    a = merge_of<64>(a);
-    if ((tid & 63) == 0) wave[tid >> 6] = {a.m, a.s, a.t};
-    __syncthreads();
-    if (tid == 0) {
-        a = merged_parts(wave, 4);
-        parts[n * slices + blockIdx.y] = {a.m, a.s, a.t};
-    }
-}
-
 template <typename T>
 __device__ __forceinline__ float logit(const LogitsView &x, int64_t n, int a)
 {
@@ -984,15 +958,128 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
     }
 }
 
+// ---- long rows, or slices of them where there are few, that are only read: a workgroup to a row (slice), a few slots of a
+// lane on their way while the ones before are added.  A lane's x are relative to the largest logit that it has seen, or to
+// 0 as long as it has seen none above.
+constexpr int kStreamSlots = 4;
+
+template <typename T, bool WITH_T>
+__device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int end, bool with_edge)
+{
+    constexpr int N = Elem<T>::N, STEP = kStreamSlots * 256;
+    const int tid = threadIdx.x;
+    Sums a;
+    a.m = 0.0f;
+    Ref ref = ref_of(a.m);
+    auto rebase = [&](float m) {
+        a = rebased(a, m, ref_of(m));
+        ref = ref_of(m);
+    };
+    auto add_one = [&](float z) {
+        const float x = ref(z), e = exp2_of(x);
+        a.s += e;
+        if (WITH_T) a.t += e * x;
+    };
+    uint4 next[kStreamSlots];
+    if (begin < end) {
+#pragma unroll
+        for (int k = 0; k < kStreamSlots; ++k) next[k] = row.load(min(begin + tid + k * 256, end - 1));
+    }
+    if (with_edge) {
+        const int e = row.edge(tid);
+        const float z = e >= 0 ? Elem<T>::load(row.p + e) : 0.0f;
+        if (z > a.m) rebase(z);
+        if (e >= 0) add_one(z);
+    }
+    for (int i = begin + tid; i - tid < end; i += STEP) {
+        uint4 v[kStreamSlots];
+#pragma unroll
+        for (int k = 0; k < kStreamSlots; ++k) v[k] = next[k];
+        if (i - tid + STEP < end) {
+#pragma unroll
+            for (int k = 0; k < kStreamSlots; ++k) next[k] = row.load(min(i + STEP + k * 256, end - 1));
+        }
+        uint32_t most = Elem<T>::kLeast;
+#pragma unroll
+        for (int k = 0; k < kStreamSlots; ++k)
+            most = Elem<T>::more(Elem<T>::more(Elem<T>::more(Elem<T>::more(most, v[k].x), v[k].y), v[k].z), v[k].w);
+        const float m = Elem<T>::largest(most);
+        if (m > a.m) rebase(m);
+#pragma unroll
+        for (int k = 0; k < kStreamSlots; ++k)
+            if (i + k * 256 < end) {
+                float f[N];
+                Elem<T>::unpack(v[k], f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) add_one(f[j]);
+            }
+    }
+    a = merge_of<64>(a);
+    if (!(a.s >= 0x1p-100f) || a.t != a.t) {             // far below 0, -infinity among them, or not a number: once more, with care
+        a = Sums{};
+        if (with_edge) {
+            const int e = row.edge(tid);
+            const float f[1] = {e >= 0 ? Elem<T>::load(row.p + e) : -INFINITY};
+            add(a, f);
+        }
+        for (int i = begin + tid; i < end; i += 256) {
+            float f[N];
+            Elem<T>::unpack(row.load(i), f);
+            add(a, f);
+        }
+        a = merge_of<64>(a);
+    }
+    return a;
+}
+
+// PASS_LOGP and PASS_PREF_FORWARD of whole rows, or (slices > 1) the sums of the slices.
+template <typename T, int PASS>
+__global__ __launch_bounds__(256) void k_stream(RowArgs g, RowPart *__restrict__ parts, int slices, bool with_t)
+{
+    __shared__ RowPart part[4];
+    const int tid = threadIdx.x;
+    for (int64_t n = blockIdx.x; n < g.x.n; n += gridDim.x) {
+        const Place p = place_of(g.rows, n);
+        const Span<T> row(static_cast<const T *>(g.x.data) + n * g.x.stride, g.x.V);
+        Sums a;
+        int act = -1;
+        float z_a = 0.0f;
+        if (p.counts) {
+            if (parts == nullptr) {
+                act = g.actions[n];
+                if (act >= 0 && act < g.x.V) z_a = Elem<T>::load(row.p + act);
+            }
+            const int per = (row.whole + slices - 1) / slices, begin = per * blockIdx.y, end = min(row.whole, begin + per);
+            a = with_t ? stream_sums<T, true>(row, begin, end, blockIdx.y == 0) : stream_sums<T, false>(row, begin, end, blockIdx.y == 0);
+            if ((tid & 63) == 0) part[tid >> 6] = {a.m, a.s, a.t};
+        }
+        __syncthreads();
+        if (tid < 64 && p.counts) {
+            const RowPart of = part[tid & 3];
+            a = merge_of<64>(tid < 4 ? Sums{of.m, of.s, of.t} : Sums{});
+        }
+        if (tid < 64) {
+            if (parts == nullptr) {
+                double none[4];
+                finish_pass<PASS>(g, n, p, a, act, z_a, tid == 0, none);
+            } else if (p.counts && tid == 0) {
+                parts[n * slices + blockIdx.y] = {a.m, a.s, a.t};
+            }
+        }
+        __syncthreads();
+    }
+}
+
 bool few_rows(const LogitsView &x) { return x.n < 64 && x.V >= 16384; }
 
 int row_blocks(int64_t n) { return static_cast<int>((n + kRowsPerBlock - 1) / kRowsPerBlock); }
 
-void launch_parts(const LogitsView &x, const RowsView &rows, const LossWorkspace &ws, hipStream_t s)
+// Sums of the slices of every row into ws.parts.
+void launch_parts(const RowArgs &g, const LossWorkspace &ws, bool with_t, hipStream_t s)
 {
-    by_type(x.dtype, [&](auto t) {
-        hipLaunchKernelGGL(k_row_parts<decltype(t)>, dim3(static_cast<uint32_t>(x.n), ws.slices), dim3(256), 0, s, x, rows, ws.parts,
-                           ws.slices);
+    by_type(g.x.dtype, [&](auto t) {
+        hipLaunchKernelGGL((k_stream<decltype(t), PASS_LOGP>), dim3(static_cast<uint32_t>(std::min<int64_t>(g.x.n, 2048)), ws.slices),
+                           dim3(256), 0, s, g, ws.parts, ws.slices, with_t);
     });
 }
 
@@ -1069,9 +1156,14 @@ int launch_rows(const RowArgs &g, hipStream_t s)
         else if (slots <= 64 * 4) go(k_rows<T, 64, 4, PASS>, 4, 256, 0, kMaxSumBlocks);
         else if (slots <= 64 * 16) go(k_rows<T, 64, 16, PASS>, 4, 256, 0, kMaxSumBlocks);
         else if (few_rows(g.x)) return;
-        else if (slots <= 256 * 16) go(k_rows<T, 256, 16, PASS>, 1, 256, 0, 1024);
-        else if (slots <= 512 * 16) go(k_rows<T, 512, 16, PASS>, 1, 512, 0, 512);
-        else if (slots <= 1024 * 16) go(k_rows<T, 1024, 16, PASS>, 1, 1024, 0, 256);
+        else if constexpr (PASS == PASS_POLICY) {
+            if (slots <= 256 * 16) go(k_rows<T, 256, 16, PASS>, 1, 256, 0, 1024);
+            else if (slots <= 512 * 16) go(k_rows<T, 512, 16, PASS>, 1, 512, 0, 2048);
+            else if (slots <= 1024 * 16) go(k_rows<T, 1024, 16, PASS>, 1, 1024, 0, 256);
+        } else {
+            blocks = static_cast<int>(std::min<int64_t>(g.x.n, 2048));
+            hipLaunchKernelGGL((k_stream<T, PASS>), dim3(blocks), dim3(256), 0, s, g, nullptr, 1, g.out_entropy != nullptr);
+        }
     });
     return blocks;
 }
@@ -1119,7 +1211,7 @@ void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_
     g.out_logp = out_logp;
     g.out_entropy = out_entropy;
     if (launch_rows<PASS_LOGP>(g, s)) return;
-    launch_parts(x, rows, ws, s);
+    launch_parts(g, ws, out_entropy != nullptr, s);
     by_type(x.dtype, [&](auto t) {
         hipLaunchKernelGGL(k_finish_logp<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, actions, ws.parts,
                            ws.slices, out_logp, out_entropy, nullptr, nullptr);
@@ -1146,7 +1238,7 @@ void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyA
             blocks = whole;
             if (blocks == 1) return;             // the kernel has written the loss
         } else {
-            launch_parts(x, rows, ws, s);
+            launch_parts(g, ws, true, s);
             by_type(x.dtype, [&](auto t) {
                 hipLaunchKernelGGL(k_finish_policy<decltype(t)>, dim3(blocks), dim3(kRowsPerBlock), 0, s, x, rows, a, ws.parts,
                                    ws.slices, ws.totals, ws.seq_n, out_grad ? ws.grad : nullptr, ws.sums);
@@ -1169,7 +1261,7 @@ void launch_preference_loss(const LogitsView &x, const RowsView &rows, const Pre
     const bool again = x.V <= kNarrow;
     if (again) g.grad = nullptr;
     if (x.n > 0 && !launch_rows<PASS_PREF_FORWARD>(g, s)) {
-        launch_parts(x, rows, ws, s);
+        launch_parts(g, ws, false, s);
         by_type(x.dtype, [&](auto t) {
             hipLaunchKernelGGL(k_finish_logp<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, a.actions,
                                ws.parts, ws.slices, a.out_logp, nullptr, ws.logp, ws.grad);
