@@ -241,25 +241,40 @@ struct PolicyRow {
     float sur = 0.0f, kl = 0.0f, H = 0.0f, cut = 0.0f;
 };
 
+// What a row has besides its logits, read before they are waited for.
+struct RowIn {
+    Place p;
+    int act = -1;
+    float adv = 0.0f, old = 0.0f, ref = 0.0f, w = 0.0f;    // w: PASS_POLICY the row's weight, PASS_PREF_GRAD d loss / d l
+};
+
+__device__ __forceinline__ void policy_in(RowIn &in, const PolicyArgs &a, const RowsView &rows, const RowTotals *totals,
+                                          const int32_t *seq_n, int64_t n)
+{
+    in.adv = a.advantages[a.advantage_per_seq ? in.p.seq : n];
+    if (a.old_logp) in.old = a.old_logp[n];
+    if (a.ref_logp) in.ref = a.ref_logp[n];
+    in.w = row_weight(rows, a.reduction, totals, seq_n, in.p.seq);
+}
+
 // Value and derivatives of a row that counts and adds something.
-__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs &a, int64_t n, int seq, float l, float H, float w)
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs &a, const RowIn &in, float l, float H)
 {
     PolicyRow r;
-    const float adv = a.advantages[a.advantage_per_seq ? seq : n];
-    const float ratio = a.old_logp ? expf(l - a.old_logp[n]) : (l == l ? 1.0f : l);
-    const bool cut = adv > 0.0f ? ratio > 1.0f + a.clip_high : (adv < 0.0f && ratio < 1.0f - a.clip_low);
-    const float held = cut ? (adv > 0.0f ? 1.0f + a.clip_high : 1.0f - a.clip_low) : ratio;
-    r.sur = w * (-adv * held);
-    r.c = cut ? 0.0f : adv * ratio;
+    const float ratio = a.old_logp ? expf(l - in.old) : (l == l ? 1.0f : l);
+    const bool cut = in.adv > 0.0f ? ratio > 1.0f + a.clip_high : (in.adv < 0.0f && ratio < 1.0f - a.clip_low);
+    const float held = cut ? (in.adv > 0.0f ? 1.0f + a.clip_high : 1.0f - a.clip_low) : ratio;
+    r.sur = in.w * (-in.adv * held);
+    r.c = cut ? 0.0f : in.adv * ratio;
     if (a.ref_logp) {
-        const float d = a.ref_logp[n] - l, e = expm1f(d);
-        r.kl = w * (e - d);
+        const float d = in.ref - l, e = expm1f(d);
+        r.kl = in.w * (e - d);
         r.c += a.kl_coeff * e;
     }
-    r.c *= w;
-    r.g = w * a.entropy_coeff;
-    r.H = w * H;
-    r.cut = cut ? w : 0.0f;
+    r.c *= in.w;
+    r.g = in.w * a.entropy_coeff;
+    r.H = in.w * H;
+    r.cut = cut ? in.w : 0.0f;
     return r;
 }
 
@@ -291,7 +306,10 @@ __global__ __launch_bounds__(kRowsPerBlock) void k_finish_policy(LogitsView x, R
             float log_s;
             finish_row(a, ok ? logit<T>(x, n, act) : 0.0f, ok, l, H, log_s);
             if (ok && l != -INFINITY && a.s != 0.0f) {
-                r = policy_row(args, n, p.seq, l, H, row_weight(rows, args.reduction, totals, seq_n, p.seq));
+                RowIn in;
+                in.p = p;
+                policy_in(in, args, rows, totals, seq_n, n);
+                r = policy_row(args, in, l, H);
                 g = grad_of(r, args, a, H, log_s);
             }
         }
@@ -426,6 +444,14 @@ __global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
     }
 }
 
+// Rows of a sequence that its bounds leave.
+__device__ __forceinline__ int bounded_length(const RowsView &rows, int q)
+{
+    if (rows.order == PL_ROWS_PACKED)
+        return static_cast<int>(max(int64_t{0}, min(rows.n, static_cast<int64_t>(rows.bounds[q + 1])) - max(0, rows.bounds[q])));
+    return rows.bounds ? min(rows.L, max(0, rows.bounds[q])) : rows.L;
+}
+
 // ---- sequences: sums of l and l - ref over the rows that count, and their number (with logp == nullptr: the
 // number only), of part blockIdx.y of every sequence: lanes_s sequences and 256 / lanes_s of their rows side by side.
 __global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *__restrict__ logp, const float *__restrict__ ref,
@@ -438,15 +464,9 @@ __global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *_
     double a = 0.0, b = 0.0;
     int c = 0;
     if (q < rows.S) {
-        int64_t first, step = 1, len;
-        if (rows.order == PL_ROWS_PACKED) {
-            first = max(0, rows.bounds[q]);
-            len = max(int64_t{0}, min(rows.n, static_cast<int64_t>(rows.bounds[q + 1])) - first);
-        } else {
-            len = rows.bounds ? min(rows.L, max(0, rows.bounds[q])) : rows.L;
-            first = rows.order == PL_ROWS_BY_STEP ? q : static_cast<int64_t>(q) * rows.L;
-            if (rows.order == PL_ROWS_BY_STEP) step = rows.S;
-        }
+        const int64_t len = bounded_length(rows, q), step = rows.order == PL_ROWS_BY_STEP ? rows.S : 1;
+        const int64_t first = rows.order == PL_ROWS_PACKED ? max(0, rows.bounds[q])
+                                                           : rows.order == PL_ROWS_BY_STEP ? q : static_cast<int64_t>(q) * rows.L;
         const int64_t per = (len + gridDim.y - 1) / gridDim.y, end = min(len, per * (blockIdx.y + 1));
 #pragma unroll 4
         for (int64_t i = per * blockIdx.y + ms; i < end; i += abreast) {
@@ -483,39 +503,50 @@ __global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *_
     }
 }
 
-// Sums of the parts of every sequence, eight lanes to one, and over all sequences (one workgroup).
-__global__ __launch_bounds__(1024) void k_seq_totals(int S, int seq_parts, const double *__restrict__ part,
+// Sums of the parts of every sequence, eight lanes to one, and over all sequences (one workgroup).  Without parts the
+// numbers of rows are those of the bounds.
+__global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, const double *__restrict__ part,
                                                      const int32_t *__restrict__ part_n, double *__restrict__ seq_sum,
                                                      int32_t *__restrict__ seq_n, RowTotals *__restrict__ totals)
 {
     __shared__ int32_t wave[16][2];
-    const int tid = threadIdx.x, lane = tid & 7;
+    const int tid = threadIdx.x, S = r.S;
     int rows = 0, seqs = 0;
-    for (int q = tid >> 3; q < S; q += 128) {
-        double a = 0.0, b = 0.0;
-        int c = 0;
-        for (int i = lane; i < seq_parts; i += 8) {
-            const size_t at = static_cast<size_t>(i) * S + q;
-            if (part) {
-                a += part[at * 2];
-                b += part[at * 2 + 1];
-            }
-            c += part_n[at];
-        }
-#pragma unroll
-        for (int o = 4; o; o >>= 1) {
-            a += __shfl_xor(a, o);
-            b += __shfl_xor(b, o);
-            c += __shfl_xor(c, o);
-        }
-        if (lane == 0) {
-            if (part) {
-                seq_sum[q * 2] = a;
-                seq_sum[q * 2 + 1] = b;
-            }
+    if (!part_n) {
+        for (int q = tid; q < S; q += 1024) {
+            const int c = bounded_length(r, q);
             seq_n[q] = c;
             rows += c;
             seqs += c > 0;
+        }
+    } else {
+        const int lane = tid & 7;
+        for (int q = tid >> 3; q < S; q += 128) {
+            double a = 0.0, b = 0.0;
+            int c = 0;
+            for (int i = lane; i < seq_parts; i += 8) {
+                const size_t at = static_cast<size_t>(i) * S + q;
+                if (part) {
+                    a += part[at * 2];
+                    b += part[at * 2 + 1];
+                }
+                c += part_n[at];
+            }
+#pragma unroll
+            for (int o = 4; o; o >>= 1) {
+                a += __shfl_xor(a, o);
+                b += __shfl_xor(b, o);
+                c += __shfl_xor(c, o);
+            }
+            if (lane == 0) {
+                if (part) {
+                    seq_sum[q * 2] = a;
+                    seq_sum[q * 2 + 1] = b;
+                }
+                seq_n[q] = c;
+                rows += c;
+                seqs += c > 0;
+            }
         }
     }
 #pragma unroll
@@ -658,16 +689,24 @@ struct RowArgs {
     int64_t grad_stride;
 };
 
+template <int PASS>
+__device__ __forceinline__ void read_in(const RowArgs &g, int64_t n, RowIn &in)
+{
+    if (!in.p.counts) return;
+    if (PASS == PASS_POLICY) policy_in(in, g.policy, g.rows, g.totals, g.seq_n, n);
+    if (PASS == PASS_PREF_GRAD) in.w = g.grad_scale * g.seq_coeff[in.p.seq];
+}
+
 // What follows from a row's sums: outputs, the row's part of the loss (added to `acc`) and its gradient.  `first`: this
 // thread writes the row's outputs and keeps its part.
 template <int PASS>
-__device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, const Place &p, const Sums &a, int act, float z_a, bool first,
+__device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, const RowIn &in, const Sums &a, float z_a, bool first,
                                                double *acc)
 {
     float l = 0.0f, H = 0.0f, log_s = 0.0f;
     bool live = false;
-    if (p.counts) {
-        const bool ok = act >= 0 && act < g.x.V;
+    if (in.p.counts) {
+        const bool ok = in.act >= 0 && in.act < g.x.V;
         finish_row(a, z_a, ok, l, H, log_s);
         live = ok && l != -INFINITY && a.s != 0.0f;
     }
@@ -675,7 +714,7 @@ __device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, cons
     if (PASS == PASS_POLICY) {
         PolicyRow r;
         if (live) {
-            r = policy_row(g.policy, n, p.seq, l, H, row_weight(g.rows, g.policy.reduction, g.totals, g.seq_n, p.seq));
+            r = policy_row(g.policy, in, l, H);
             rg = grad_of(r, g.policy, a, H, log_s);
         }
         if (first) {
@@ -688,7 +727,7 @@ __device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, cons
         }
     }
     if (PASS == PASS_PREF_GRAD) {
-        const float c = live ? g.grad_scale * g.seq_coeff[p.seq] : 0.0f;
+        const float c = live ? in.w : 0.0f;
         rg.C = c;
         rg.A = c == 0.0f ? 0.0f : -c / a.s;
         if (first && g.out_coeff) g.out_coeff[n] = -c;
@@ -763,7 +802,8 @@ __device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, in
     }
 }
 
-template <typename T, int PASS>
+// CAP > 0: rows of up to CAP actions, which the thread keeps in registers.
+template <typename T, int PASS, int CAP>
 __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
 {
     extern __shared__ float tile[];
@@ -773,32 +813,51 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
     for (int64_t n0 = static_cast<int64_t>(blockIdx.x) * 256; n0 < g.x.n; n0 += static_cast<int64_t>(gridDim.x) * 256) {
         const int count = static_cast<int>(min(int64_t{256}, g.x.n - n0));
+        const int64_t n = n0 + tid;
+        RowIn in;
+        in.p.counts = false;
+        if (tid < count) {
+            in.p = place_of(g.rows, n);
+            if (in.p.counts) in.act = g.actions[n];
+            read_in<PASS>(g, n, in);
+        }
         narrow_tile<T, false>(g.x.data, g.x.stride, n0, count, V, g.magic, pitch, tile);
         __syncthreads();
         if (tid < count) {
-            const int64_t n = n0 + tid;
             float *z = tile + tid * pitch;
+            float reg[CAP > 0 ? CAP : 1];
             Sums a;
-            const Place p = place_of(g.rows, n);
-            const int act = p.counts ? g.actions[n] : -1;
-            if (p.counts) {
-                for (int j = 0; j < V; ++j) a.m = fmaxf(a.m, z[j]);
+            // f(j, logit j) for every action
+            auto each = [&](auto f) {
+                if (CAP > 0) {
+#pragma unroll
+                    for (int j = 0; j < CAP; ++j)
+                        if (j < V) f(j, reg[j]);
+                } else {
+                    for (int j = 0; j < V; ++j) f(j, z[j]);
+                }
+            };
+#pragma unroll
+            for (int j = 0; j < CAP; ++j)
+                if (j < V) reg[j] = z[j];
+            if (in.p.counts) {
+                each([&](int, float v) { a.m = fmaxf(a.m, v); });
                 const Ref ref = ref_of(a.m);
-                for (int j = 0; j < V; ++j) {
-                    const float x = ref(z[j]), e = exp2_of(x);
+                each([&](int, float v) {
+                    const float x = ref(v), e = exp2_of(x);
                     a.s += e;
                     a.t += e * fmaxf(x, kLowest);
-                }
+                });
             }
-            const RowGrad rg = finish_pass<PASS>(g, n, p, a, act, act >= 0 && act < V ? z[act] : 0.0f, true, acc);
+            const RowGrad rg = finish_pass<PASS>(g, n, in, a, in.act >= 0 && in.act < V ? z[in.act] : 0.0f, true, acc);
             if (kGrad && g.out_grad) {
                 const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
                 const Ref ref = ref_of(rg.m);
-                for (int j = 0; j < V; ++j) {
-                    float f[1] = {z[j]};
+                each([&](int j, float v) {
+                    float f[1] = {v};
                     grad_slot<1>(f, rg, ref);
-                    z[j] = none ? 0.0f : f[0] + (j == act ? rg.C : 0.0f);
-                }
+                    z[j] = none ? 0.0f : f[0] + (j == in.act ? rg.C : 0.0f);
+                });
             }
         }
         __syncthreads();
@@ -844,13 +903,16 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
         asm volatile("" : "+v"(lane));               // the slots' offsets are taken anew: kept over the rows they would cost CH registers
         const Span<T> row(static_cast<const T *>(g.x.data) + n * g.x.stride, V);
         const int head = row.head, whole = row.whole, edge = row.edge(lane);
-        const Place p = place_of(g.rows, n);
-        const int act = p.counts ? g.actions[n] : -1;
+        RowIn in;
+        in.p = place_of(g.rows, n);
+        if (in.p.counts) in.act = g.actions[n];
+        if (WAVES <= 1 || tid < 64) read_in<PASS>(g, n, in);
+        const int act = in.act;
         const bool acts = act >= 0 && act < V;
         uint4 v[CH];
         float z_edge = -INFINITY, z_a = 0.0f;
         Sums a;
-        if (p.counts) {
+        if (in.p.counts) {
 #pragma unroll
             for (int k = 0; k < CH; ++k)
                 if (k * LANES < whole) v[k] = row.load(k * LANES + lane);
@@ -909,13 +971,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
             if (tid < 64) {
                 const RowPart of = part[lane < WAVES ? lane : 0];
                 a = merge_of<64>(lane < WAVES ? Sums{of.m, of.s, of.t} : Sums{});
-                rg = finish_pass<PASS>(g, n, p, a, act, z_a, tid == 0, loss[0]);
+                rg = finish_pass<PASS>(g, n, in, a, z_a, tid == 0, loss[0]);
                 if (tid == 0) shared_grad = rg;
             }
             __syncthreads();
             rg = shared_grad;
         } else {
-            rg = finish_pass<PASS>(g, n, p, a, act, z_a, lane == 0, loss[mine]);
+            rg = finish_pass<PASS>(g, n, in, a, z_a, lane == 0, loss[mine]);
         }
         if (kGrad && g.out_grad) {
             T *o = static_cast<T *>(g.out_grad) + n * g.grad_stride;
@@ -1039,30 +1101,30 @@ __global__ __launch_bounds__(256) void k_stream(RowArgs g, RowPart *__restrict__
     __shared__ RowPart part[4];
     const int tid = threadIdx.x;
     for (int64_t n = blockIdx.x; n < g.x.n; n += gridDim.x) {
-        const Place p = place_of(g.rows, n);
+        RowIn in;
+        in.p = place_of(g.rows, n);
         const Span<T> row(static_cast<const T *>(g.x.data) + n * g.x.stride, g.x.V);
         Sums a;
-        int act = -1;
         float z_a = 0.0f;
-        if (p.counts) {
+        if (in.p.counts) {
             if (parts == nullptr) {
-                act = g.actions[n];
-                if (act >= 0 && act < g.x.V) z_a = Elem<T>::load(row.p + act);
+                in.act = g.actions[n];
+                if (in.act >= 0 && in.act < g.x.V) z_a = Elem<T>::load(row.p + in.act);
             }
             const int per = (row.whole + slices - 1) / slices, begin = per * blockIdx.y, end = min(row.whole, begin + per);
             a = with_t ? stream_sums<T, true>(row, begin, end, blockIdx.y == 0) : stream_sums<T, false>(row, begin, end, blockIdx.y == 0);
             if ((tid & 63) == 0) part[tid >> 6] = {a.m, a.s, a.t};
         }
         __syncthreads();
-        if (tid < 64 && p.counts) {
+        if (tid < 64 && in.p.counts) {
             const RowPart of = part[tid & 3];
             a = merge_of<64>(tid < 4 ? Sums{of.m, of.s, of.t} : Sums{});
         }
         if (tid < 64) {
             if (parts == nullptr) {
                 double none[4];
-                finish_pass<PASS>(g, n, p, a, act, z_a, tid == 0, none);
-            } else if (p.counts && tid == 0) {
+                finish_pass<PASS>(g, n, in, a, z_a, tid == 0, none);
+            } else if (in.p.counts && tid == 0) {
                 parts[n * slices + blockIdx.y] = {a.m, a.s, a.t};
             }
         }
@@ -1114,16 +1176,27 @@ int seq_lanes(const RowsView &rows)
     return lanes;
 }
 
-// Sums and numbers of rows of every sequence (logp), or their numbers and how many rows and sequences count in all.
+// Sums and numbers of rows of every sequence.
 void launch_seq_sums(const RowsView &rows, const double *logp, const float *ref, const LossWorkspace &ws, hipStream_t s)
 {
     const int lanes_s = seq_lanes(rows);
-    const bool whole = logp && ws.seq_parts == 1;
+    const bool whole = ws.seq_parts == 1;
     hipLaunchKernelGGL(k_seq_sums, dim3((rows.S + lanes_s - 1) / lanes_s, ws.seq_parts), dim3(256), 0, s, rows, logp, ref,
-                       lanes_s, whole ? ws.seq_sum : logp ? ws.seq_part : nullptr, whole ? ws.seq_n : ws.seq_part_n);
+                       lanes_s, whole ? ws.seq_sum : ws.seq_part, whole ? ws.seq_n : ws.seq_part_n);
     if (!whole)
-        hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows.S, ws.seq_parts, logp ? ws.seq_part : nullptr, ws.seq_part_n,
-                           ws.seq_sum, ws.seq_n, ws.totals);
+        hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows, ws.seq_parts, ws.seq_part, ws.seq_part_n, ws.seq_sum, ws.seq_n,
+                           ws.totals);
+}
+
+// Numbers of rows of every sequence, and how many rows and sequences count in all.
+void launch_seq_counts(const RowsView &rows, const LossWorkspace &ws, hipStream_t s)
+{
+    const int lanes_s = seq_lanes(rows);
+    if (rows.mask)
+        hipLaunchKernelGGL(k_seq_sums, dim3((rows.S + lanes_s - 1) / lanes_s, ws.seq_parts), dim3(256), 0, s, rows, nullptr, nullptr,
+                           lanes_s, nullptr, ws.seq_part_n);
+    hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows, ws.seq_parts, nullptr, rows.mask ? ws.seq_part_n : nullptr, nullptr,
+                       ws.seq_n, ws.totals);
 }
 
 RowArgs row_args(const LogitsView &x, const RowsView &rows, const int32_t *actions)
@@ -1149,7 +1222,15 @@ int launch_rows(const RowArgs &g, hipStream_t s)
             blocks = static_cast<int>(std::min<int64_t>((g.x.n + rows - 1) / rows, most));
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, g);
         };
-        if (g.x.V <= kNarrow) go(k_narrow<T, PASS>, 256, 256, 256 * (g.x.V | 1) * sizeof(float), kMaxSumBlocks);
+        if (g.x.V <= kNarrow) {
+            // as many rounds for every workgroup
+            const int64_t tiles = row_blocks(g.x.n), rounds = (tiles + kMaxSumBlocks - 1) / kMaxSumBlocks;
+            const int most = static_cast<int>((tiles + rounds - 1) / rounds);
+            const size_t lds = 256 * (g.x.V | 1) * sizeof(float);
+            if (g.x.V <= 8) go(k_narrow<T, PASS, 8>, 256, 256, lds, most);
+            else if (g.x.V <= 16) go(k_narrow<T, PASS, 16>, 256, 256, lds, most);
+            else go(k_narrow<T, PASS, 0>, 256, 256, lds, most);
+        }
         if constexpr (PASS == PASS_PREF_GRAD) return;
         else if (g.x.V <= kNarrow) return;
         else if (slots <= 16 * 2) go(k_rows<T, 16, 2, PASS>, 16, 256, 0, kMaxSumBlocks);
@@ -1157,11 +1238,11 @@ int launch_rows(const RowArgs &g, hipStream_t s)
         else if (slots <= 64 * 16) go(k_rows<T, 64, 16, PASS>, 4, 256, 0, kMaxSumBlocks);
         else if (few_rows(g.x)) return;
         else if constexpr (PASS == PASS_POLICY) {
-            if (slots <= 256 * 16) go(k_rows<T, 256, 16, PASS>, 1, 256, 0, 1024);
-            else if (slots <= 512 * 16) go(k_rows<T, 512, 16, PASS>, 1, 512, 0, 2048);
-            else if (slots <= 1024 * 16) go(k_rows<T, 1024, 16, PASS>, 1, 1024, 0, 256);
+            if (slots <= 256 * 16) go(k_rows<T, 256, 16, PASS>, 1, 256, 0, kMaxSumBlocks);
+            else if (slots <= 512 * 16) go(k_rows<T, 512, 16, PASS>, 1, 512, 0, kMaxSumBlocks);
+            else if (slots <= 1024 * 16) go(k_rows<T, 1024, 16, PASS>, 1, 1024, 0, kMaxSumBlocks);
         } else {
-            blocks = static_cast<int>(std::min<int64_t>(g.x.n, 2048));
+            blocks = static_cast<int>(std::min<int64_t>(g.x.n, 1 << 22));
             hipLaunchKernelGGL((k_stream<T, PASS>), dim3(blocks), dim3(256), 0, s, g, nullptr, 1, g.out_entropy != nullptr);
         }
     });
@@ -1221,7 +1302,7 @@ void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_
 void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, float *out_stats, void *out_grad,
                         int64_t grad_stride, const LossWorkspace &ws, hipStream_t s)
 {
-    if (x.n > 0 && !rows.all && a.reduction != PL_REDUCE_SUM) launch_seq_sums(rows, nullptr, nullptr, ws, s);
+    if (x.n > 0 && !rows.all && a.reduction != PL_REDUCE_SUM) launch_seq_counts(rows, ws, s);
     int blocks = row_blocks(x.n);
     if (x.n > 0) {
         RowArgs g = row_args(x, rows, a.actions);
