@@ -46,6 +46,14 @@ int view_rows(const pl_rows *in, const LogitsView &x, RowsView *r)
         if (x.n % in->n_seqs) return fail(PL_ERR_SHAPE, "n_rows must be a multiple of n_seqs");
         r->L = static_cast<int>(x.n / in->n_seqs);
     }
+    // division by a constant: with 2^(b-1) < q <= 2^b, n / q = n * ceil(2^(31+b) / q) / 2^(31+b) for every n < 2^31
+    const uint32_t q = in->order == PL_ROWS_BY_STEP ? static_cast<uint32_t>(r->S) : static_cast<uint32_t>(r->L);
+    if (q > 1) {
+        int b = 1;
+        while ((uint64_t{1} << b) < q) ++b;
+        r->magic = static_cast<uint32_t>(((uint64_t{1} << (31 + b)) + q - 1) / q);
+        r->shift = b - 1;
+    }
     r->bounds = in->bounds;
     r->mask = in->mask;
     r->all = !in->bounds && !in->mask;
@@ -128,8 +136,8 @@ int pl_clipped_policy_loss(const pl_logits *logits, const pl_rows *rows_in, cons
     if (!out_stats || (x.n > 0 && !advantages)) return fail(PL_ERR_NULL, "advantages and out_stats are required");
     const PolicyArgs a{actions, advantages, old_logp, ref_logp, out_logp, out_entropy, out_coeff, out_entropy_coeff,
                        cfg->clip_low, cfg->clip_high, cfg->kl_coeff, cfg->entropy_coeff, cfg->grad_scale,
-                       cfg->reduction, cfg->advantage_per_seq};
-    launch_policy_loss(x, rows, a, out_stats, out_grad, grad_stride, ws, static_cast<hipStream_t>(stream));
+                       cfg->advantage_per_seq, 1.0f, nullptr, nullptr};
+    launch_policy_loss(x, rows, a, cfg->reduction, out_stats, out_grad, grad_stride, ws, static_cast<hipStream_t>(stream));
     PL_HIP(hipGetLastError());
     return PL_OK;
 }

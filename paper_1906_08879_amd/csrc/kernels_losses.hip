@@ -154,7 +154,8 @@ __device__ __forceinline__ Place place_of(const RowsView &r, int64_t n)
         p.counts = r.bounds[lo] <= n && n < r.bounds[lo + 1];
     } else {
         const int q = r.order == PL_ROWS_BY_STEP ? r.S : r.L;
-        const int u = static_cast<int>(static_cast<uint32_t>(n) / static_cast<uint32_t>(q)), v = static_cast<int>(n) - u * q;
+        const int u = r.magic ? static_cast<int>(__umulhi(static_cast<uint32_t>(n), r.magic) >> r.shift) : static_cast<int>(n);
+        const int v = static_cast<int>(n) - u * q;
         p.seq = r.order == PL_ROWS_BY_STEP ? v : u;
         const int step = r.order == PL_ROWS_BY_STEP ? u : v;
         if (r.bounds) p.counts = step < r.bounds[p.seq];
@@ -178,13 +179,20 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
+// 1 / s to an ulp, for s that is neither tiny nor huge.
+__device__ __forceinline__ float reciprocal(float s)
+{
+    const float r = __builtin_amdgcn_rcpf(s);
+    return __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
+}
+
 // l, H and log s of a row from its sums; a row without an allowed action has l = NaN, an action of probability zero
 // l = -infinity.
 __device__ __forceinline__ void finish_row(const Sums &a, float z_a, bool action_ok, float &l, float &H, float &log_s)
 {
     const float log2_s = log2f(a.s);
     log_s = kLn2 * log2_s;
-    H = kLn2 * (log2_s - a.t / a.s);
+    H = kLn2 * (log2_s - a.t * reciprocal(a.s));
     l = !action_ok ? NAN : far_out(a.m) ? (z_a - a.m) - log_s : kLn2 * (ref_of(a.m)(z_a) - log2_s);
     if (a.s == 0.0f) H = l = NAN;
 }
@@ -226,16 +234,6 @@ __global__ __launch_bounds__(kRowsPerBlock) void k_finish_logp(LogitsView x, Row
     if (grad) grad[n] = g;
 }
 
-// Weight of a row that counts.
-__device__ __forceinline__ float row_weight(const RowsView &rows, int reduction, const RowTotals *totals, const int32_t *seq_n,
-                                            int seq)
-{
-    if (reduction == PL_REDUCE_SUM) return 1.0f;
-    if (reduction == PL_REDUCE_ROWS) return 1.0f / static_cast<float>(rows.all ? static_cast<int32_t>(rows.n) : totals->rows);
-    if (rows.all) return static_cast<float>(1.0 / (static_cast<double>(rows.S) * rows.L));
-    return static_cast<float>(1.0 / (static_cast<double>(totals->seqs) * seq_n[seq]));
-}
-
 struct PolicyRow {
     float c = 0.0f, g = 0.0f;          // - d loss / d l, - d loss / d H, without the gradient's scale
     float sur = 0.0f, kl = 0.0f, H = 0.0f, cut = 0.0f;
@@ -248,13 +246,12 @@ struct RowIn {
     float adv = 0.0f, old = 0.0f, ref = 0.0f, w = 0.0f;    // w: PASS_POLICY the row's weight, PASS_PREF_GRAD d loss / d l
 };
 
-__device__ __forceinline__ void policy_in(RowIn &in, const PolicyArgs &a, const RowsView &rows, const RowTotals *totals,
-                                          const int32_t *seq_n, int64_t n)
+__device__ __forceinline__ void policy_in(RowIn &in, const PolicyArgs &a, int64_t n)
 {
     in.adv = a.advantages[a.advantage_per_seq ? in.p.seq : n];
     if (a.old_logp) in.old = a.old_logp[n];
     if (a.ref_logp) in.ref = a.ref_logp[n];
-    in.w = row_weight(rows, a.reduction, totals, seq_n, in.p.seq);
+    in.w = a.weights ? a.weights[in.p.seq] : a.weight_at ? *a.weight_at : a.weight;
 }
 
 // Value and derivatives of a row that counts and adds something.
@@ -281,15 +278,14 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs &a, const RowIn
 __device__ __forceinline__ RowGrad grad_of(const PolicyRow &r, const PolicyArgs &a, const Sums &sums, float H, float log_s)
 {
     const float c = -r.c * a.grad_scale, g = r.g * a.grad_scale;
-    return {sums.m, (-c + g * (H - log_s)) / sums.s, kLn2 * g / sums.s, c};
+    const float per = reciprocal(sums.s);
+    return {sums.m, (-c + g * (H - log_s)) * per, kLn2 * g * per, c};
 }
 
 template <typename T>
 __global__ __launch_bounds__(kRowsPerBlock) void k_finish_policy(LogitsView x, RowsView rows, PolicyArgs args,
                                                                  const RowPart *__restrict__ parts, int slices,
-                                                                 const RowTotals *__restrict__ totals,
-                                                                 const int32_t *__restrict__ seq_n, RowGrad *__restrict__ grad,
-                                                                 double *__restrict__ sums)
+                                                                 RowGrad *__restrict__ grad, double *__restrict__ sums)
 {
     const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + threadIdx.x;
     const int tid = threadIdx.x;
@@ -308,7 +304,7 @@ __global__ __launch_bounds__(kRowsPerBlock) void k_finish_policy(LogitsView x, R
             if (ok && l != -INFINITY && a.s != 0.0f) {
                 RowIn in;
                 in.p = p;
-                policy_in(in, args, rows, totals, seq_n, n);
+                policy_in(in, args, n);
                 r = policy_row(args, in, l, H);
                 g = grad_of(r, args, a, H, log_s);
             }
@@ -349,21 +345,21 @@ __device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g, const
 }
 
 // ---- the loss from the workgroups' sums, in their order
-__global__ __launch_bounds__(256) void k_policy_stats(const double *__restrict__ sums, int blocks, float kl_coeff,
-                                                      float entropy_coeff, float *__restrict__ out)
+__global__ __launch_bounds__(1024) void k_policy_stats(const double *__restrict__ sums, int blocks, float kl_coeff,
+                                                       float entropy_coeff, float *__restrict__ out)
 {
-    __shared__ double wave[4][4];
     const int tid = threadIdx.x;
-    double v[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int b = tid; b < blocks; b += 256)
-        for (int i = 0; i < 4; ++i) v[i] += sums[static_cast<size_t>(b) * 4 + i];
-    for (int i = 0; i < 4; ++i) {
-        v[i] = wave_sum(v[i]);
-        if ((tid & 63) == 0) wave[tid >> 6][i] = v[i];
-    }
+    double a = 0.0;                              // of sum tid & 3
+    for (int64_t i = tid; i < static_cast<int64_t>(blocks) * 4; i += 1024) a += sums[i];
+#pragma unroll
+    for (int o = 32; o >= 4; o >>= 1) a += __shfl_xor(a, o);
+    __shared__ double last[16][4];
+    if ((tid & 63) < 4) last[tid >> 6][tid & 3] = a;
     __syncthreads();
     if (tid == 0) {
-        for (int i = 0; i < 4; ++i) v[i] = wave[0][i] + wave[1][i] + wave[2][i] + wave[3][i];
+        double v[4] = {0.0, 0.0, 0.0, 0.0};
+        for (int w = 0; w < 16; ++w)
+            for (int i = 0; i < 4; ++i) v[i] += last[w][i];
         policy_stats_out(v, kl_coeff, entropy_coeff, out);
     }
 }
@@ -503,11 +499,12 @@ __global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *_
     }
 }
 
-// Sums of the parts of every sequence, eight lanes to one, and over all sequences (one workgroup).  Without parts the
-// numbers of rows are those of the bounds.
+// Sums of the parts of every sequence, eight lanes to one (one workgroup).  Without parts the numbers of rows are those of
+// the bounds.  And the weights of rows: `weight` of any, `weights` of those of each sequence.
 __global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, const double *__restrict__ part,
                                                      const int32_t *__restrict__ part_n, double *__restrict__ seq_sum,
-                                                     int32_t *__restrict__ seq_n, RowTotals *__restrict__ totals)
+                                                     int32_t *__restrict__ seq_n, float *__restrict__ weight,
+                                                     float *__restrict__ weights)
 {
     __shared__ int32_t wave[16][2];
     const int tid = threadIdx.x, S = r.S;
@@ -559,13 +556,17 @@ __global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, 
         wave[tid >> 6][1] = seqs;
     }
     __syncthreads();
-    if (tid == 0) {
-        for (int i = 1; i < 16; ++i) {
-            rows += wave[i][0];
-            seqs += wave[i][1];
-        }
-        *totals = {rows, seqs};
+    rows = seqs = 0;
+    for (int i = 0; i < 16; ++i) {
+        rows += wave[i][0];
+        seqs += wave[i][1];
     }
+    if (weight && tid == 0) *weight = rows > 0 ? 1.0f / static_cast<float>(rows) : 0.0f;
+    if (weights)
+        for (int q = tid; q < S; q += 1024) {
+            const int c = seq_n[q];
+            weights[q] = c > 0 ? static_cast<float>(1.0 / (static_cast<double>(seqs) * c)) : 0.0f;
+        }
 }
 
 // ---- pairs: margins, the loss, and d loss / d s of every sequence
@@ -676,8 +677,6 @@ struct RowArgs {
     const int32_t *actions;
     float *out_logp, *out_entropy;
     PolicyArgs policy;                 // PASS_POLICY
-    const RowTotals *totals;
-    const int32_t *seq_n;
     double *sums;
     float *out_stats;
     double *logp;                      // PASS_PREF_FORWARD
@@ -693,7 +692,7 @@ template <int PASS>
 __device__ __forceinline__ void read_in(const RowArgs &g, int64_t n, RowIn &in)
 {
     if (!in.p.counts) return;
-    if (PASS == PASS_POLICY) policy_in(in, g.policy, g.rows, g.totals, g.seq_n, n);
+    if (PASS == PASS_POLICY) policy_in(in, g.policy, n);
     if (PASS == PASS_PREF_GRAD) in.w = g.grad_scale * g.seq_coeff[in.p.seq];
 }
 
@@ -729,7 +728,7 @@ __device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, cons
     if (PASS == PASS_PREF_GRAD) {
         const float c = live ? in.w : 0.0f;
         rg.C = c;
-        rg.A = c == 0.0f ? 0.0f : -c / a.s;
+        rg.A = c == 0.0f ? 0.0f : -c * reciprocal(a.s);
         if (first && g.out_coeff) g.out_coeff[n] = -c;
     } else if (first) {
         if (g.out_logp) g.out_logp[n] = l;
@@ -802,77 +801,112 @@ __device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, in
     }
 }
 
-// CAP > 0: rows of up to CAP actions, which the thread keeps in registers.
-template <typename T, int PASS, int CAP>
+// CAP > 0: the thread keeps its row in CAP registers.  WHOLE: rows of CAP actions are whole slots of 16 aligned bytes, which
+// the thread reads and writes itself, without LDS (rows of 8 floats, 800k of them: this, against CAP = 16 through LDS,
+// is what the last step of launch_rows measured).
+template <typename T, int PASS, int CAP, bool WHOLE>
 __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
 {
-    extern __shared__ float tile[];
-    __shared__ double wave[4][4];
+    constexpr int N = Elem<T>::N;
     constexpr bool kGrad = PASS == PASS_POLICY || PASS == PASS_PREF_GRAD;
-    const int V = g.x.V, pitch = V | 1, tid = threadIdx.x;
+    extern __shared__ float tile[];
+    __shared__ double sums[4][PASS == PASS_POLICY ? 256 : 1];
+    const int V = WHOLE ? CAP : g.x.V, pitch = V | 1, tid = threadIdx.x;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 256, n = n0 + tid;
+    const int count = static_cast<int>(min(int64_t{256}, g.x.n - n0));
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int64_t n0 = static_cast<int64_t>(blockIdx.x) * 256; n0 < g.x.n; n0 += static_cast<int64_t>(gridDim.x) * 256) {
-        const int count = static_cast<int>(min(int64_t{256}, g.x.n - n0));
-        const int64_t n = n0 + tid;
-        RowIn in;
-        in.p.counts = false;
-        if (tid < count) {
-            in.p = place_of(g.rows, n);
-            if (in.p.counts) in.act = g.actions[n];
-            read_in<PASS>(g, n, in);
-        }
-        narrow_tile<T, false>(g.x.data, g.x.stride, n0, count, V, g.magic, pitch, tile);
-        __syncthreads();
-        if (tid < count) {
-            float *z = tile + tid * pitch;
-            float reg[CAP > 0 ? CAP : 1];
-            Sums a;
-            // f(j, logit j) for every action
-            auto each = [&](auto f) {
-                if (CAP > 0) {
-#pragma unroll
-                    for (int j = 0; j < CAP; ++j)
-                        if (j < V) f(j, reg[j]);
-                } else {
-                    for (int j = 0; j < V; ++j) f(j, z[j]);
-                }
-            };
+    RowIn in;
+    in.p.counts = false;
+    if (tid < count) {
+        in.p = place_of(g.rows, n);
+        if (in.p.counts) in.act = g.actions[n];
+        read_in<PASS>(g, n, in);
+    }
+    float reg[CAP > 0 ? CAP : 1];
+    float *z = tile + tid * pitch;
+    // f(j, logit j) for every action
+    auto each = [&](auto f) {
+        if (CAP > 0) {
 #pragma unroll
             for (int j = 0; j < CAP; ++j)
-                if (j < V) reg[j] = z[j];
-            if (in.p.counts) {
-                each([&](int, float v) { a.m = fmaxf(a.m, v); });
-                const Ref ref = ref_of(a.m);
-                each([&](int, float v) {
-                    const float x = ref(v), e = exp2_of(x);
-                    a.s += e;
-                    a.t += e * fmaxf(x, kLowest);
-                });
-            }
-            const RowGrad rg = finish_pass<PASS>(g, n, in, a, in.act >= 0 && in.act < V ? z[in.act] : 0.0f, true, acc);
-            if (kGrad && g.out_grad) {
-                const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
-                const Ref ref = ref_of(rg.m);
-                each([&](int j, float v) {
-                    float f[1] = {v};
-                    grad_slot<1>(f, rg, ref);
-                    z[j] = none ? 0.0f : f[0] + (j == in.act ? rg.C : 0.0f);
-                });
+                if (WHOLE || j < V) f(j, reg[j]);
+        } else {
+            for (int j = 0; j < V; ++j) f(j, z[j]);
+        }
+    };
+    if (WHOLE) {
+        if (in.p.counts) {
+            const uint4 *at = reinterpret_cast<const uint4 *>(static_cast<const T *>(g.x.data) + n * g.x.stride);
+#pragma unroll
+            for (int i = 0; i < CAP / N; ++i) {
+                float f[N];
+                Elem<T>::unpack(at[i], f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) reg[i * N + j] = f[j];
             }
         }
+    } else {
+        narrow_tile<T, false>(g.x.data, g.x.stride, n0, count, V, g.magic, pitch, tile);
         __syncthreads();
+#pragma unroll
+        for (int j = 0; j < CAP; ++j)
+            if (j < V) reg[j] = z[j];
+    }
+    if (tid < count) {
+        Sums a;
+        float z_a = 0.0f;
+        if (in.p.counts) {
+            each([&](int, float v) { a.m = fmaxf(a.m, v); });
+            const Ref ref = ref_of(a.m);
+            each([&](int j, float v) {
+                const float x = ref(v), e = exp2_of(x);
+                a.s += e;
+                a.t += e * fmaxf(x, kLowest);
+                if (j == in.act) z_a = v;
+            });
+        }
+        const RowGrad rg = finish_pass<PASS>(g, n, in, a, z_a, true, acc);
         if (kGrad && g.out_grad) {
-            narrow_tile<T, true>(g.out_grad, g.grad_stride, n0, count, V, g.magic, pitch, tile);
-            __syncthreads();
+            const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
+            const Ref ref = ref_of(rg.m);
+            auto gradient = [&](int j, float v) {
+                float f[1] = {v};
+                grad_slot<1>(f, rg, ref);
+                return none ? 0.0f : f[0] + (j == in.act ? rg.C : 0.0f);
+            };
+            if (WHOLE) {
+                T *out = static_cast<T *>(g.out_grad) + n * g.grad_stride;
+#pragma unroll
+                for (int i = 0; i < CAP / N; ++i) {
+                    float f[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) f[j] = gradient(i * N + j, reg[i * N + j]);
+                    *reinterpret_cast<uint4 *>(out + i * N) = Elem<T>::pack(f);
+                }
+            } else {
+                each([&](int j, float v) { z[j] = gradient(j, v); });
+            }
         }
     }
-    if (PASS == PASS_POLICY) {
-        for (int i = 0; i < 4; ++i) {
-            const double v = wave_sum(acc[i]);
-            if ((tid & 63) == 0) wave[tid >> 6][i] = v;
-        }
+    if (kGrad && !WHOLE && g.out_grad) {
         __syncthreads();
-        finish_sums(g, wave, 4);
+        narrow_tile<T, true>(g.out_grad, g.grad_stride, n0, count, V, g.magic, pitch, tile);
+    }
+    if (PASS == PASS_POLICY) {
+        for (int i = 0; i < 4; ++i) sums[i][tid] = acc[i];
+        __syncthreads();
+        const int i = tid >> 6, lane = tid & 63;         // wave i takes sum i
+        const double v = wave_sum((sums[i][lane] + sums[i][lane + 64]) + (sums[i][lane + 128] + sums[i][lane + 192]));
+        if (gridDim.x > 1) {
+            if (lane == 0) g.sums[static_cast<size_t>(blockIdx.x) * 4 + i] = v;
+        } else {                                         // nobody else has sums
+            if (lane == 0) sums[i][0] = v;
+            __syncthreads();
+            if (tid == 0) {
+                const double all[4] = {sums[0][0], sums[1][0], sums[2][0], sums[3][0]};
+                policy_stats_out(all, g.policy.ref_logp ? g.policy.kl_coeff : 0.0f, g.policy.entropy_coeff, g.out_stats);
+            }
+        }
     }
 }
 
@@ -906,7 +940,6 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
         RowIn in;
         in.p = place_of(g.rows, n);
         if (in.p.counts) in.act = g.actions[n];
-        if (WAVES <= 1 || tid < 64) read_in<PASS>(g, n, in);
         const int act = in.act;
         const bool acts = act >= 0 && act < V;
         uint4 v[CH];
@@ -964,6 +997,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
                 a = merge_of<G>(a);
             }
         }
+        if (WAVES <= 1 || tid < 64) read_in<PASS>(g, n, in);
         RowGrad rg;
         if (WAVES > 1) {
             if ((tid & 63) == 0) part[tid >> 6] = {a.m, a.s, a.t};
@@ -1185,18 +1219,18 @@ void launch_seq_sums(const RowsView &rows, const double *logp, const float *ref,
                        lanes_s, whole ? ws.seq_sum : ws.seq_part, whole ? ws.seq_n : ws.seq_part_n);
     if (!whole)
         hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows, ws.seq_parts, ws.seq_part, ws.seq_part_n, ws.seq_sum, ws.seq_n,
-                           ws.totals);
+                           nullptr, nullptr);
 }
 
-// Numbers of rows of every sequence, and how many rows and sequences count in all.
-void launch_seq_counts(const RowsView &rows, const LossWorkspace &ws, hipStream_t s)
+// The weights of rows whose number is found on the device.
+void launch_weights(const RowsView &rows, bool by_seqs, const LossWorkspace &ws, hipStream_t s)
 {
     const int lanes_s = seq_lanes(rows);
     if (rows.mask)
         hipLaunchKernelGGL(k_seq_sums, dim3((rows.S + lanes_s - 1) / lanes_s, ws.seq_parts), dim3(256), 0, s, rows, nullptr, nullptr,
                            lanes_s, nullptr, ws.seq_part_n);
     hipLaunchKernelGGL(k_seq_totals, dim3(1), dim3(1024), 0, s, rows, ws.seq_parts, nullptr, rows.mask ? ws.seq_part_n : nullptr, nullptr,
-                       ws.seq_n, ws.totals);
+                       ws.seq_n, by_seqs ? nullptr : ws.weight, by_seqs ? ws.weights : nullptr);
 }
 
 RowArgs row_args(const LogitsView &x, const RowsView &rows, const int32_t *actions)
@@ -1223,13 +1257,14 @@ int launch_rows(const RowArgs &g, hipStream_t s)
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, g);
         };
         if (g.x.V <= kNarrow) {
-            // as many rounds for every workgroup
-            const int64_t tiles = row_blocks(g.x.n), rounds = (tiles + kMaxSumBlocks - 1) / kMaxSumBlocks;
-            const int most = static_cast<int>((tiles + rounds - 1) / rounds);
+            constexpr int N = Elem<T>::N;
+            const bool at_16 = (reinterpret_cast<uintptr_t>(g.x.data) | reinterpret_cast<uintptr_t>(g.out_grad)) % 16 == 0 &&
+                               g.x.stride % N == 0 && (!g.out_grad || g.grad_stride % N == 0);
             const size_t lds = 256 * (g.x.V | 1) * sizeof(float);
-            if (g.x.V <= 8) go(k_narrow<T, PASS, 8>, 256, 256, lds, most);
-            else if (g.x.V <= 16) go(k_narrow<T, PASS, 16>, 256, 256, lds, most);
-            else go(k_narrow<T, PASS, 0>, 256, 256, lds, most);
+            if (at_16 && g.x.V == N) go(k_narrow<T, PASS, N, true>, 256, 256, 0, 1 << 23);
+            else if (at_16 && g.x.V == 2 * N) go(k_narrow<T, PASS, 2 * N, true>, 256, 256, 0, 1 << 23);
+            else if (g.x.V <= 16) go(k_narrow<T, PASS, 16, false>, 256, 256, lds, 1 << 23);
+            else go(k_narrow<T, PASS, 0, false>, 256, 256, lds, 1 << 23);
         }
         if constexpr (PASS == PASS_PREF_GRAD) return;
         else if (g.x.V <= kNarrow) return;
@@ -1276,7 +1311,8 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
     take(w.seq_sum, S * 2);
     take(w.seq_n, S);
     take(w.seq_coeff, S);
-    take(w.totals, 1);
+    take(w.weights, S);
+    take(w.weight, 1);
     take(w.sums, static_cast<size_t>(std::max(row_blocks(x.n), kMaxSumBlocks)) * 4);
     w.bytes = pos;
     return w;
@@ -1299,18 +1335,24 @@ void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_
     });
 }
 
-void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, float *out_stats, void *out_grad,
-                        int64_t grad_stride, const LossWorkspace &ws, hipStream_t s)
+void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &args, int reduction, float *out_stats,
+                        void *out_grad, int64_t grad_stride, const LossWorkspace &ws, hipStream_t s)
 {
-    if (x.n > 0 && !rows.all && a.reduction != PL_REDUCE_SUM) launch_seq_counts(rows, ws, s);
+    PolicyArgs a = args;
+    if (x.n > 0 && reduction != PL_REDUCE_SUM) {
+        if (rows.all) {
+            a.weight = static_cast<float>(1.0 / static_cast<double>(x.n));   // sequences of equal length: the same for both
+        } else {
+            launch_weights(rows, reduction == PL_REDUCE_SEQS, ws, s);
+            (reduction == PL_REDUCE_SEQS ? a.weights : a.weight_at) = reduction == PL_REDUCE_SEQS ? ws.weights : ws.weight;
+        }
+    }
     int blocks = row_blocks(x.n);
     if (x.n > 0) {
         RowArgs g = row_args(x, rows, a.actions);
         g.policy = a;
         g.out_logp = a.out_logp;
         g.out_entropy = a.out_entropy;
-        g.totals = ws.totals;
-        g.seq_n = ws.seq_n;
         g.sums = ws.sums;
         g.out_stats = out_stats;
         g.out_grad = out_grad;
@@ -1322,12 +1364,12 @@ void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyA
             launch_parts(g, ws, true, s);
             by_type(x.dtype, [&](auto t) {
                 hipLaunchKernelGGL(k_finish_policy<decltype(t)>, dim3(blocks), dim3(kRowsPerBlock), 0, s, x, rows, a, ws.parts,
-                                   ws.slices, ws.totals, ws.seq_n, out_grad ? ws.grad : nullptr, ws.sums);
+                                   ws.slices, out_grad ? ws.grad : nullptr, ws.sums);
             });
             if (out_grad) launch_grad(grad_args(x, a.actions, ws, out_grad, grad_stride), s);
         }
     }
-    hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(256), 0, s, ws.sums, blocks, a.ref_logp ? a.kl_coeff : 0.0f,
+    hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, ws.sums, blocks, a.ref_logp ? a.kl_coeff : 0.0f,
                        a.entropy_coeff, out_stats);
 }
 

@@ -27,12 +27,9 @@ struct RowsView {
     const uint8_t *mask = nullptr;
     int64_t n = 0;
     int S = 1, L = 0, order = PL_ROWS_BY_SEQ;
+    uint32_t magic = 0;                // n / (S or L) = high word of n * magic, shifted right (for n < 2^31; 0: divided by 1)
+    int shift = 0;
     bool all = true;                   // every row counts, known on the host
-};
-
-// Rows that count, and sequences with such rows.
-struct RowTotals {
-    int32_t rows, seqs;
 };
 
 // Maximum m and sums over a slice of a row: of 2^x and of 2^x x, x = k z - o with k and o from m (ref_of).
@@ -51,7 +48,10 @@ struct PolicyArgs {
     const float *advantages, *old_logp, *ref_logp;
     float *out_logp, *out_entropy, *out_coeff, *out_entropy_coeff;
     float clip_low, clip_high, kl_coeff, entropy_coeff, grad_scale;
-    int reduction, advantage_per_seq;
+    int advantage_per_seq;
+    float weight;                      // of a row, unless
+    const float *weights;              // there is one for each sequence, or
+    const float *weight_at;            // it is found on the device
 };
 
 struct PrefArgs {
@@ -73,8 +73,9 @@ struct LossWorkspace {
     double *seq_sum = nullptr;         // [S, 2]
     int32_t *seq_n = nullptr;          // [S]
     float *seq_coeff = nullptr;        // [S]
-    RowTotals *totals = nullptr;       // [1]
-    double *sums = nullptr;            // [workgroups, 4], at most kMaxSumBlocks or one per kRowsPerBlock rows
+    float *weights = nullptr;          // [S], for PL_REDUCE_SEQS
+    float *weight = nullptr;           // [1], for PL_REDUCE_ROWS
+    double *sums = nullptr;            // [workgroups, 4]: kMaxSumBlocks, or one for kRowsPerBlock rows
     int slices = 1, seq_parts = 1;
     size_t bytes = 0;
 };
@@ -84,8 +85,8 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
 // csrc/kernels_losses.hip
 void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_logp, float *out_entropy,
                         const LossWorkspace &ws, hipStream_t s);
-void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, float *out_stats, void *out_grad,
-                        int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
+void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, int reduction, float *out_stats,
+                        void *out_grad, int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
 void launch_preference_loss(const LogitsView &x, const RowsView &rows, const PrefArgs &a, float *out_stats, void *out_grad,
                             int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
 
