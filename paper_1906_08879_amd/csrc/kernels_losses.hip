@@ -350,6 +350,7 @@ __global__ __launch_bounds__(1024) void k_policy_stats(const double *__restrict_
 {
     const int tid = threadIdx.x;
     double a = 0.0;                              // of sum tid & 3
+#pragma unroll 8
     for (int64_t i = tid; i < static_cast<int64_t>(blocks) * 4; i += 1024) a += sums[i];
 #pragma unroll
     for (int o = 32; o >= 4; o >>= 1) a += __shfl_xor(a, o);
@@ -449,57 +450,89 @@ __device__ __forceinline__ int bounded_length(const RowsView &rows, int q)
 }
 
 // ---- sequences: sums of l and l - ref over the rows that count, and their number (with logp == nullptr: the
-// number only), of part blockIdx.y of every sequence: lanes_s sequences and 256 / lanes_s of their rows side by side.
-__global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *__restrict__ logp, const float *__restrict__ ref,
-                                                  int lanes_s, double *__restrict__ part, int32_t *__restrict__ part_n)
+// number only)
+struct SeqSum {
+    double l = 0.0, ratio = 0.0;
+    int n = 0;
+};
+
+// Steps i, i + by, ... below `end` of sequence q.
+__device__ __forceinline__ SeqSum add_steps(const RowsView &rows, const double *__restrict__ logp, const float *__restrict__ ref, int q,
+                                            int64_t i, int64_t end, int by)
 {
-    __shared__ double sum[256][2];
-    __shared__ int32_t cnt[256];
-    const int tid = threadIdx.x, ls = tid & (lanes_s - 1), ms = tid / lanes_s, abreast = 256 / lanes_s;
-    const int q = blockIdx.x * lanes_s + ls;
-    double a = 0.0, b = 0.0;
-    int c = 0;
-    if (q < rows.S) {
-        const int64_t len = bounded_length(rows, q), step = rows.order == PL_ROWS_BY_STEP ? rows.S : 1;
-        const int64_t first = rows.order == PL_ROWS_PACKED ? max(0, rows.bounds[q])
-                                                           : rows.order == PL_ROWS_BY_STEP ? q : static_cast<int64_t>(q) * rows.L;
-        const int64_t per = (len + gridDim.y - 1) / gridDim.y, end = min(len, per * (blockIdx.y + 1));
-#pragma unroll 4
-        for (int64_t i = per * blockIdx.y + ms; i < end; i += abreast) {
-            const int64_t n = first + i * step;
-            const bool in = !rows.mask || rows.mask[n];
-            c += in;
-            if (!logp) continue;
-            const double l = logp[n];
-            const float r = ref ? ref[n] : 0.0f;
-            if (in && l != kAddsNothing) {
-                a += l;
-                b += l - r;
+    SeqSum s;
+    const int64_t step = rows.order == PL_ROWS_BY_STEP ? rows.S : 1;
+    const int64_t first = rows.order == PL_ROWS_PACKED ? max(0, rows.bounds[q])
+                                                       : rows.order == PL_ROWS_BY_STEP ? q : static_cast<int64_t>(q) * rows.L;
+    // (eight rows at a time, their loads together: past the end the last one again)
+    for (; i < end; i += 8 * by) {
+        double l[8];
+        float r[8];
+        bool in[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t at = i + k * by, n = first + min(at, end - 1) * step;
+            in[k] = at < end && (!rows.mask || rows.mask[n]);
+            l[k] = logp ? logp[n] : 0.0;
+            r[k] = logp && ref ? ref[n] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            s.n += in[k];
+            if (in[k] && l[k] != kAddsNothing) {
+                s.l += l[k];
+                s.ratio += l[k] - r[k];
             }
         }
     }
-    sum[tid][0] = a;
-    sum[tid][1] = b;
-    cnt[tid] = c;
-    for (int o = 128; o >= lanes_s; o >>= 1) {
+    return s;
+}
+
+// Sums over the threads of a workgroup whose numbers are equal modulo lanes_s, for the first lanes_s of them.
+template <int THREADS>
+__device__ __forceinline__ SeqSum sum_abreast(SeqSum s, int lanes_s)
+{
+    __shared__ double l[THREADS], ratio[THREADS];
+    __shared__ int n[THREADS];
+    const int tid = threadIdx.x;
+    __syncthreads();
+    l[tid] = s.l;
+    ratio[tid] = s.ratio;
+    n[tid] = s.n;
+    for (int o = THREADS / 2; o >= lanes_s; o >>= 1) {
         __syncthreads();
         if (tid < o) {
-            sum[tid][0] += sum[tid + o][0];
-            sum[tid][1] += sum[tid + o][1];
-            cnt[tid] += cnt[tid + o];
+            l[tid] += l[tid + o];
+            ratio[tid] += ratio[tid + o];
+            n[tid] += n[tid + o];
         }
     }
+    return {l[tid], ratio[tid], n[tid]};
+}
+
+// Part blockIdx.y of every sequence: lanes_s sequences and 256 / lanes_s of their rows side by side.
+__global__ __launch_bounds__(256) void k_seq_sums(RowsView rows, const double *__restrict__ logp, const float *__restrict__ ref,
+                                                  int lanes_s, double *__restrict__ part, int32_t *__restrict__ part_n)
+{
+    const int tid = threadIdx.x, ls = tid & (lanes_s - 1), abreast = 256 / lanes_s;
+    const int q = blockIdx.x * lanes_s + ls;
+    SeqSum s;
+    if (q < rows.S) {
+        const int64_t len = bounded_length(rows, q), per = (len + gridDim.y - 1) / gridDim.y;
+        s = add_steps(rows, logp, ref, q, per * blockIdx.y + tid / lanes_s, min(len, per * (blockIdx.y + 1)), abreast);
+    }
+    s = sum_abreast<256>(s, lanes_s);
     if (tid < lanes_s && q < rows.S) {
         const size_t at = static_cast<size_t>(blockIdx.y) * rows.S + q;
         if (part) {
-            part[at * 2] = sum[tid][0];
-            part[at * 2 + 1] = sum[tid][1];
+            part[at * 2] = s.l;
+            part[at * 2 + 1] = s.ratio;
         }
-        part_n[at] = cnt[tid];
+        part_n[at] = s.n;
     }
 }
 
-// Sums of the parts of every sequence, eight lanes to one (one workgroup).  Without parts the numbers of rows are those of
+// Sums of the parts of every sequence, sixteen lanes to one (one workgroup).  Without parts the numbers of rows are those of
 // the bounds.  And the weights of rows: `weight` of any, `weights` of those of each sequence.
 __global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, const double *__restrict__ part,
                                                      const int32_t *__restrict__ part_n, double *__restrict__ seq_sum,
@@ -517,11 +550,12 @@ __global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, 
             seqs += c > 0;
         }
     } else {
-        const int lane = tid & 7;
-        for (int q = tid >> 3; q < S; q += 128) {
+        const int lane = tid & 15;
+        for (int q = tid >> 4; q < S; q += 64) {
             double a = 0.0, b = 0.0;
             int c = 0;
-            for (int i = lane; i < seq_parts; i += 8) {
+#pragma unroll 4
+            for (int i = lane; i < seq_parts; i += 16) {
                 const size_t at = static_cast<size_t>(i) * S + q;
                 if (part) {
                     a += part[at * 2];
@@ -530,7 +564,7 @@ __global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, 
                 c += part_n[at];
             }
 #pragma unroll
-            for (int o = 4; o; o >>= 1) {
+            for (int o = 8; o; o >>= 1) {
                 a += __shfl_xor(a, o);
                 b += __shfl_xor(b, o);
                 c += __shfl_xor(c, o);
@@ -599,21 +633,24 @@ __device__ __forceinline__ float d_margin(float m, float eps)
 
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))) + (x != x ? x : 0.0f); }
 
-// A thread per sequence.  With a list of pairs every workgroup goes over all of them, 256 at a time through LDS, and adds
-// those of its sequences in the pairs' order; without one a sequence is in one pair.  The first workgroup adds up the loss.
-__global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *__restrict__ seq_sum,
-                                               const int32_t *__restrict__ seq_n, float *__restrict__ seq_coeff,
-                                               float *__restrict__ out_stats)
+// d loss / d s of the THREADS / kTeam sequences from q0 on, kTeam lanes to each: with a list of pairs they go over all of
+// them, THREADS at a time through LDS, and add those of their sequence; without one a sequence is in one pair.  `first`:
+// the loss and the margins as well.
+constexpr int kTeam = 8;
+
+template <int THREADS>
+__device__ __forceinline__ void pairs_of(const PrefArgs &p, int S, int q0, bool first, const double *seq_sum, const int32_t *seq_n,
+                                         float *__restrict__ seq_coeff, float *__restrict__ out_stats)
 {
-    __shared__ int4 tile[256];
-    __shared__ double wave[4][3];
-    const int tid = threadIdx.x, q = blockIdx.x * 256 + tid;
+    __shared__ int4 tile[THREADS];
+    __shared__ double wave[THREADS / 64][3];
+    const int tid = threadIdx.x, lane = tid & (kTeam - 1), q = q0 + tid / kTeam;
     double loss = 0.0, right = 0.0, valid = 0.0, coeff = 0.0;
     auto margin = [&](const Pair &pr) {
         return static_cast<float>(p.beta * (seq_ratio(p, seq_sum, seq_n, pr.a, 1) - seq_ratio(p, seq_sum, seq_n, pr.b, 1)));
     };
-    if (p.pairs || blockIdx.x == 0)
-        for (int i0 = 0; i0 < p.n_pairs; i0 += 256) {
+    if (p.pairs || first)
+        for (int i0 = 0; i0 < p.n_pairs; i0 += THREADS) {
             const int i = i0 + tid;
             Pair pr{-1, -1, false};
             float m = NAN, g = 0.0f;
@@ -622,40 +659,57 @@ __global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *
                 if (pr.ok) {
                     m = margin(pr);
                     g = d_margin(m, p.smoothing);
-                    loss += (1.0f - p.smoothing) * softplus(-m) + p.smoothing * softplus(m);
+                    if (first) loss += (1.0f - p.smoothing) * softplus(-m) + p.smoothing * softplus(m);
                     right += m > 0.0f;
                     valid += 1.0;
                 }
-                if (blockIdx.x == 0 && p.out_margins) p.out_margins[i] = m;
+                if (first && p.out_margins) p.out_margins[i] = m;
             }
             if (!p.pairs) continue;
             __syncthreads();
             tile[tid] = {pr.ok ? pr.a : -1, pr.ok ? pr.b : -1, __float_as_int(g), 0};
             __syncthreads();
-            const int n = min(256, p.n_pairs - i0);
+            const int n = min(THREADS, p.n_pairs - i0);
 #pragma unroll 8
-            for (int k = 0; k < n; ++k) {
+            for (int k = lane; k < n; k += kTeam) {
                 const int4 e = tile[k];
-                const float v = __int_as_float(e.z);
-                coeff += (e.x == q ? v : 0.0f) - (e.y == q ? v : 0.0f);
+                if (e.x == q || e.y == q) coeff += (e.x == q ? __int_as_float(e.z) : 0.0f) - (e.y == q ? __int_as_float(e.z) : 0.0f);
             }
         }
-    loss = wave_sum(loss);
-    right = wave_sum(right);
-    valid = wave_sum(valid);
-    if ((tid & 63) == 0) {
-        wave[tid >> 6][0] = loss;
-        wave[tid >> 6][1] = right;
-        wave[tid >> 6][2] = valid;
+    if (p.pairs || first) {                              // (the same for the whole workgroup)
+        __shared__ double all[3];
+        if (first) {
+            loss = wave_sum(loss);
+            right = wave_sum(right);
+        }
+        valid = wave_sum(valid);
+        __syncthreads();
+        if ((tid & 63) == 0) {
+            wave[tid >> 6][0] = loss;
+            wave[tid >> 6][1] = right;
+            wave[tid >> 6][2] = valid;
+        }
+        __syncthreads();
+        if (tid < 3) {
+            double v = 0.0;
+#pragma unroll
+            for (int w = 0; w < THREADS / 64; ++w) v += wave[w][tid];
+            all[tid] = v;
+        }
+        __syncthreads();
+        loss = all[0];
+        right = all[1];
+        valid = all[2];
     }
-    __syncthreads();
-    valid = p.pairs ? wave[0][2] + wave[1][2] + wave[2][2] + wave[3][2] : p.n_pairs;
+    if (!p.pairs) valid = p.n_pairs;
     const double per = valid > 0.0 ? 1.0 / valid : 0.0;
-    if (blockIdx.x == 0 && tid == 0) {
-        out_stats[0] = static_cast<float>((wave[0][0] + wave[1][0] + wave[2][0] + wave[3][0]) * per);
-        out_stats[1] = static_cast<float>((wave[0][1] + wave[1][1] + wave[2][1] + wave[3][1]) * per);
+    if (first && tid == 0) {
+        out_stats[0] = static_cast<float>(loss * per);
+        out_stats[1] = static_cast<float>(right * per);
     }
-    if (q < S) {
+#pragma unroll
+    for (int o = kTeam / 2; o; o >>= 1) coeff += __shfl_xor(coeff, o);
+    if (lane == 0 && q < S) {
         if (!p.pairs && (q >> 1) < p.n_pairs) {
             const float g = d_margin(margin(Pair{q & ~1, q | 1, true}), p.smoothing);
             coeff = (q & 1) ? -g : g;
@@ -665,6 +719,49 @@ __global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *
         seq_coeff[q] = static_cast<float>(coeff);
         if (p.out_seq_logp) p.out_seq_logp[q] = static_cast<float>(seq_ratio(p, seq_sum, seq_n, q, 0));
     }
+}
+
+__global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *__restrict__ seq_sum, const int32_t *__restrict__ seq_n,
+                                               float *__restrict__ seq_coeff, float *__restrict__ out_stats)
+{
+    pairs_of<256>(p, S, blockIdx.x * (256 / kTeam), blockIdx.x == 0, seq_sum, seq_n, seq_coeff, out_stats);
+}
+
+// Few rows: the sums of sequences and the pairs in one launch by one workgroup (instead of three).
+__global__ __launch_bounds__(1024) void k_pref_middle(RowsView rows, PrefArgs p, const double *__restrict__ logp, int lanes_s,
+                                                      float *__restrict__ seq_coeff, float *__restrict__ out_stats)
+{
+    __shared__ double seq_sum[2 * kMiddleSeqs];
+    __shared__ int32_t seq_n[kMiddleSeqs];
+    const int tid = threadIdx.x;
+    if (rows.order == PL_ROWS_BY_STEP) {
+        for (int q0 = 0; q0 < rows.S; q0 += lanes_s) {
+            const int q = q0 + (tid & (lanes_s - 1));
+            SeqSum s;
+            if (q < rows.S) s = add_steps(rows, logp, p.ref_logp, q, tid / lanes_s, bounded_length(rows, q), 1024 / lanes_s);
+            s = sum_abreast<1024>(s, lanes_s);
+            if (tid < lanes_s && q < rows.S) {
+                seq_sum[q * 2] = s.l;
+                seq_sum[q * 2 + 1] = s.ratio;
+                seq_n[q] = s.n;
+            }
+        }
+    } else {                                             // a wave to a sequence
+        for (int q = tid >> 6; q < rows.S; q += 16) {
+            SeqSum s = add_steps(rows, logp, p.ref_logp, q, tid & 63, bounded_length(rows, q), 64);
+            s.l = wave_sum(s.l);
+            s.ratio = wave_sum(s.ratio);
+#pragma unroll
+            for (int o = 32; o; o >>= 1) s.n += __shfl_xor(s.n, o);
+            if ((tid & 63) == 0) {
+                seq_sum[q * 2] = s.l;
+                seq_sum[q * 2 + 1] = s.ratio;
+                seq_n[q] = s.n;
+            }
+        }
+    }
+    __syncthreads();
+    for (int q0 = 0; q0 < rows.S; q0 += 1024 / kTeam) pairs_of<1024>(p, rows.S, q0, q0 == 0, seq_sum, seq_n, seq_coeff, out_stats);
 }
 
 // What a kernel that takes whole rows does with them.
@@ -1189,6 +1286,14 @@ void launch_grad(GradArgs a, hipStream_t s)
     });
 }
 
+// Whether one workgroup does the sums of sequences and the pairs.  By step, its threads share a sequence's rows (64 sequences
+// of 200 steps: 19 us a call against 25 with three launches); otherwise a wave has a sequence to itself, which is slower
+// than two launches more (24 sequences of 256 rows: 18 us against 10) unless they are very few.
+bool middle_fits(const RowsView &rows)
+{
+    return rows.S <= kMiddleSeqs && rows.n <= (rows.order == PL_ROWS_BY_STEP ? kMiddleRows : kMiddleRows / 16);
+}
+
 GradArgs grad_args(const LogitsView &x, const int32_t *actions, const LossWorkspace &ws, void *out, int64_t out_stride)
 {
     GradArgs a{};
@@ -1299,9 +1404,9 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
     // a thousand workgroups where the rows are fewer, of 8192 logits at least
     if (x.n > 0)    // (the workspace does not depend on which kernels run)
         w.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({1024 / x.n, x.V / 8192, kMaxSlices})));
-    // sixteen rows to a thread of k_seq_sums, as long as the workgroups are few
+    // eight rows to a thread of k_seq_sums, as long as the workgroups are few
     const int64_t longest = rows.order == PL_ROWS_PACKED ? rows.n / rows.S : rows.L;
-    const int64_t per_part = 16 * (256 / seq_lanes(rows)), groups = (rows.S + seq_lanes(rows) - 1) / seq_lanes(rows);
+    const int64_t per_part = 8 * (256 / seq_lanes(rows)), groups = (rows.S + seq_lanes(rows) - 1) / seq_lanes(rows);
     w.seq_parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({(longest + per_part - 1) / per_part, kMaxSeqParts, 2048 / groups})));
     take(w.parts, n * w.slices);
     take(w.grad, n);
@@ -1390,8 +1495,13 @@ void launch_preference_loss(const LogitsView &x, const RowsView &rows, const Pre
                                ws.parts, ws.slices, a.out_logp, nullptr, ws.logp, ws.grad);
         });
     }
-    launch_seq_sums(rows, ws.logp, a.ref_logp, ws, s);
-    hipLaunchKernelGGL(k_pairs, dim3((rows.S + 255) / 256), dim3(256), 0, s, a, rows.S, ws.seq_sum, ws.seq_n, ws.seq_coeff, out_stats);
+    if (middle_fits(rows)) {
+        hipLaunchKernelGGL(k_pref_middle, dim3(1), dim3(1024), 0, s, rows, a, ws.logp, seq_lanes(rows), ws.seq_coeff, out_stats);
+    } else {
+        launch_seq_sums(rows, ws.logp, a.ref_logp, ws, s);
+        hipLaunchKernelGGL(k_pairs, dim3((rows.S + 256 / kTeam - 1) / (256 / kTeam)), dim3(256), 0, s, a, rows.S, ws.seq_sum, ws.seq_n,
+                           ws.seq_coeff, out_stats);
+    }
     if (x.n == 0 || (!out_grad && !a.out_coeff)) return;
     if (again) {
         g.out_coeff = a.out_coeff;
