@@ -13,11 +13,21 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 
 typedef short shortx2 __attribute__((ext_vector_type(2)));
+typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 
 // Two 16-bit elements of a word side by side.
 __device__ __forceinline__ uint32_t more_of_two(uint32_t a, uint32_t b)
 {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(shortx2, a), __builtin_bit_cast(shortx2, b)));
+}
+
+__device__ __forceinline__ uint32_t less_of_two(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(ushortx2, a), __builtin_bit_cast(ushortx2, b)));
+}
+__device__ __forceinline__ uint32_t largest_of_two(uint32_t most, uint32_t least)
+{
+    return ((most & 0x8000u ? least : most) & 0xffffu) | ((most & 0x80000000u ? least : most) & 0xffff0000u);
 }
 
 template <typename T>
@@ -33,11 +43,15 @@ struct Elem<float> {
     {
         return {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
     }
-    // The largest of values among which one is not negative has the largest bits as a signed number: a word's worth of
-    // elements with one integer instruction.
-    static constexpr uint32_t kLeast = 0x80000000u;
+    // The largest of values among which one is not negative has the largest bits as a signed number, the largest of
+    // negative ones the least as an unsigned number: a word's worth of elements with an integer instruction each.
+    static constexpr uint32_t kNone = 0x80000000u;       // `more` of nothing; `less` of nothing is 0xffffffff, a NaN
     static __device__ uint32_t more(uint32_t a, uint32_t b) { return static_cast<uint32_t>(max(static_cast<int32_t>(a), static_cast<int32_t>(b))); }
-    static __device__ float largest(uint32_t a) { return __uint_as_float(a); }
+    static __device__ uint32_t less(uint32_t a, uint32_t b) { return min(a, b); }
+    static __device__ float largest(uint32_t most, uint32_t least)
+    {
+        return __uint_as_float(static_cast<int32_t>(most) < 0 ? least : most);
+    }
     static __device__ float load(const float *p) { return *p; }
     static __device__ void store(float *p, float f) { *p = f; }
 };
@@ -61,10 +75,12 @@ struct Elem<__bf16> {
             w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){f[2 * i], f[2 * i + 1]}, bf16x2));
         return {w[0], w[1], w[2], w[3]};
     }
-    static constexpr uint32_t kLeast = 0x80008000u;
+    static constexpr uint32_t kNone = 0x80008000u;
     static __device__ uint32_t more(uint32_t a, uint32_t b) { return more_of_two(a, b); }
-    static __device__ float largest(uint32_t a)
+    static __device__ uint32_t less(uint32_t a, uint32_t b) { return less_of_two(a, b); }
+    static __device__ float largest(uint32_t most, uint32_t least)
     {
+        const uint32_t a = largest_of_two(most, least);
         return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
     }
     static __device__ float load(const __bf16 *p) { return static_cast<float>(*p); }
@@ -91,11 +107,13 @@ struct Elem<_Float16> {
             w[i] = __builtin_bit_cast(uint32_t, (halfx2){static_cast<_Float16>(f[2 * i]), static_cast<_Float16>(f[2 * i + 1])});
         return {w[0], w[1], w[2], w[3]};
     }
-    static constexpr uint32_t kLeast = 0x80008000u;
+    static constexpr uint32_t kNone = 0x80008000u;
     static __device__ uint32_t more(uint32_t a, uint32_t b) { return more_of_two(a, b); }
-    static __device__ float largest(uint32_t a)
+    static __device__ uint32_t less(uint32_t a, uint32_t b) { return less_of_two(a, b); }
+    static __device__ float largest(uint32_t most, uint32_t least)
     {
-        return fmaxf(static_cast<float>(__builtin_bit_cast(halfx2, a).x), static_cast<float>(__builtin_bit_cast(halfx2, a).y));
+        const halfx2 a = __builtin_bit_cast(halfx2, largest_of_two(most, least));
+        return fmaxf(static_cast<float>(a.x), static_cast<float>(a.y));
     }
     static __device__ float load(const _Float16 *p) { return static_cast<float>(*p); }
     static __device__ void store(_Float16 *p, float f) { *p = static_cast<_Float16>(f); }

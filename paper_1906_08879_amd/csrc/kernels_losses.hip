@@ -1,14 +1,13 @@
 // Losses on rows of logits (include/placeto.h): log probabilities of actions, the clipped policy loss
 // and the preference loss, with the gradient of the logits.
 //
-// For a row z with maximum m, in powers of two: x_j = k z_j - o with k = log2 e and o = k m, rounded,
-// s = sum_j 2^{x_j} and t = sum_j 2^{x_j} x_j give
-//     l = log pi(a) = ln 2 (x_a - log2 s),      H = ln 2 (log2 s - t / s),
+// For a row z with maximum m, in powers of two: x_j = (z_j - m) log2 e, s = sum_j 2^{x_j} and t = sum_j 2^{x_j} x_j give
+//     l = log pi(a) = (z_a - m) - ln 2 log2 s,      H = ln 2 (log2 s - t / s),
 // and with w c = d loss / d l and -w g = d loss / d H the gradient of logit j is
 //     w [ c (1[j = a] - p_j) + g p_j (log p_j + H) ] = 2^{x_j} (A + B x_j) + C 1[j = a],
 //     C = w c,  B = ln 2 w g / s,  A = (-w c + w g (H - ln s)) / s.
-// x_j is one fused multiply-add, rounded once however far the row lies from zero: the rounding of o is the same for
-// every j and drops out of all three, that of k is a temperature of 1 + 2^-26.
+// z_j - m is taken before it is scaled: it is exact near the maximum, however far the row lies from zero, so that a
+// probability close to 1 has a logarithm close to 0 (one fused multiply-add for both leaves that at 1e-7).
 #include <algorithm>
 #include <cmath>
 
@@ -24,20 +23,12 @@ constexpr float kLowest = -300.0f;     // 2^-300 is 0 in fp32: an x below it sta
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// z -> x of a maximum m.  (A row of -infinity alone has sums of 0.)
 struct Ref {
-    float k, o;
-    __device__ float operator()(float z) const { return __builtin_fmaf(z, k, -o); }
+    float m;
+    __device__ float operator()(float z) const { return (z - m) * kLog2e; }
 };
-
-// k and o of a maximum.  Past 2^126 logits are 2^103 apart or equal: with a smaller k, k m is an fp32 number, and
-// the differences are still far below any 2^x that is not 0.  A row of -infinity alone has sums of 0.
-__device__ __forceinline__ bool far_out(float m) { return fabsf(m) >= 0x1p126f; }
-__device__ __forceinline__ Ref ref_of(float m)
-{
-    if (m == -INFINITY) return {kLog2e, 0.0f};
-    const float k = far_out(m) ? 0x1p-20f : kLog2e;
-    return {k, m * k};
-}
+__device__ __forceinline__ Ref ref_of(float m) { return {m == -INFINITY ? 0.0f : m}; }
 
 // ---- over 16 lanes (a DPP row) and over a wave
 template <int CTRL>
@@ -92,7 +83,7 @@ struct Sums {
 __device__ __forceinline__ Sums rebased(const Sums &a, float m, const Ref &to)
 {
     if (a.s == 0.0f) return {m, 0.0f, 0.0f};
-    const float d = ref_of(a.m).o - to.o, e = exp2_of(d);
+    const float d = to(ref_of(a.m).m), e = exp2_of(d);
     return {m, a.s * e, e * (a.t + fmaxf(d, kLowest) * a.s)};
 }
 
@@ -110,22 +101,6 @@ __device__ __forceinline__ Sums merge_of(const Sums &a)
     const float m = max_of<LANES>(a.m);
     const Sums x = rebased(a, m, ref_of(m));
     return {m, sum_of<LANES>(x.s), sum_of<LANES>(x.t)};
-}
-
-template <int N>
-__device__ __forceinline__ void add(Sums &a, const float (&f)[N])
-{
-    float m = a.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, f[i]);
-    const Ref to = ref_of(m);
-    if (m != a.m) a = rebased(a, m, to);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float x = to(f[i]), e = exp2_of(x);
-        a.s += e;
-        a.t += e * fmaxf(x, kLowest);
-    }
 }
 
 __device__ __forceinline__ Sums merged_parts(const RowPart *parts, int slices)
@@ -167,9 +142,7 @@ __device__ __forceinline__ Place place_of(const RowsView &r, int64_t n)
 // l of a row to more than fp32: the sums over a sequence, whose difference to another one's counts, see no rounding of l.
 __device__ __forceinline__ double exact_l(const Sums &a, float z_a)
 {
-    const Ref ref = ref_of(a.m);
-    if (far_out(a.m)) return (static_cast<double>(z_a) - a.m) - log(static_cast<double>(a.s));
-    return 0.69314718055994530942 * ((static_cast<double>(z_a) * ref.k - ref.o) - log2(static_cast<double>(a.s)));
+    return (static_cast<double>(z_a) - a.m) - log(static_cast<double>(a.s));
 }
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -193,7 +166,7 @@ __device__ __forceinline__ void finish_row(const Sums &a, float z_a, bool action
     const float log2_s = log2f(a.s);
     log_s = kLn2 * log2_s;
     H = kLn2 * (log2_s - a.t * reciprocal(a.s));
-    l = !action_ok ? NAN : far_out(a.m) ? (z_a - a.m) - log_s : kLn2 * (ref_of(a.m)(z_a) - log2_s);
+    l = action_ok ? (z_a - a.m) - log_s : NAN;
     if (a.s == 0.0f) H = l = NAN;
 }
 
@@ -1007,6 +980,14 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
     }
 }
 
+// The words of a slot into the candidates for the largest logit.
+template <typename T>
+__device__ __forceinline__ void add_words(const uint4 &v, uint32_t &most, uint32_t &least)
+{
+    most = Elem<T>::more(Elem<T>::more(Elem<T>::more(Elem<T>::more(most, v.x), v.y), v.z), v.w);
+    least = Elem<T>::less(Elem<T>::less(Elem<T>::less(Elem<T>::less(least, v.x), v.y), v.z), v.w);
+}
+
 // The slot stays in its four registers: without this the compiler keeps every unpacked value from one use to the next.
 __device__ __forceinline__ void keep_packed(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
@@ -1049,23 +1030,17 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
             if (edge >= 0) z_edge = Elem<T>::load(row.p + edge);
             if (acts) z_a = Elem<T>::load(row.p + act);
             constexpr int G = LANES < 64 ? LANES : 64;
-            uint32_t most[2] = {Elem<T>::kLeast, Elem<T>::kLeast};
+            uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (k * LANES < whole) {
-                    most[0] = Elem<T>::more(Elem<T>::more(most[0], v[k].x), v[k].y);
-                    most[1] = Elem<T>::more(Elem<T>::more(most[1], v[k].z), v[k].w);
-                }
-            // x is taken relative to the largest logit, or to 0 where all are negative: that is as good, unless they are far
-            // below
-            a.m = max_of<G>(fmaxf(z_edge, Elem<T>::largest(Elem<T>::more(most[0], most[1]))));
-            if (__float_as_int(a.m) < 0) a.m = 0.0f;
+                if (k * LANES < whole) add_words<T>(v[k], most, least);
+            a.m = max_of<G>(fmaxf(z_edge, Elem<T>::largest(most, least)));
             const Ref ref = ref_of(a.m);
             auto add_all = [&](auto with_t) {
                 auto add_one = [&](float z) {
                     const float x = ref(z), e = exp2_of(x);
                     a.s += e;
-                    if (with_t) a.t += e * x;
+                    if (with_t) a.t += e * fmaxf(x, kLowest);
                 };
                 if (edge >= 0) add_one(z_edge);
 #pragma unroll
@@ -1083,16 +1058,6 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
             };
             if (PASS == PASS_POLICY || (PASS == PASS_LOGP && g.out_entropy)) add_all(std::true_type{});
             else add_all(std::false_type{});
-            if (!(a.s >= 0x1p-100f) || a.t != a.t) {     // far below 0, -infinity among them, or not a number: once more, with care
-                a = Sums{};
-                const Row<T> again(g.x.data, g.x.stride, n, V);
-                for (int i = WAVES > 1 ? tid : lane; i < again.slots; i += LANES) {
-                    float f[N];
-                    again.load(i, f, -INFINITY);
-                    add(a, f);
-                }
-                a = merge_of<G>(a);
-            }
         }
         if (WAVES <= 1 || tid < 64) read_in<PASS>(g, n, in);
         RowGrad rg;
@@ -1152,8 +1117,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
 }
 
 // ---- long rows, or slices of them where there are few, that are only read: a workgroup to a row (slice), a few slots of a
-// lane on their way while the ones before are added.  A lane's x are relative to the largest logit that it has seen, or to
-// 0 as long as it has seen none above.
+// lane on their way while the ones before are added.  A lane's x are relative to the largest logit that it has seen.
 constexpr int kStreamSlots = 4;
 
 template <typename T, bool WITH_T>
@@ -1162,7 +1126,6 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
     constexpr int N = Elem<T>::N, STEP = kStreamSlots * 256;
     const int tid = threadIdx.x;
     Sums a;
-    a.m = 0.0f;
     Ref ref = ref_of(a.m);
     auto rebase = [&](float m) {
         a = rebased(a, m, ref_of(m));
@@ -1171,7 +1134,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
     auto add_one = [&](float z) {
         const float x = ref(z), e = exp2_of(x);
         a.s += e;
-        if (WITH_T) a.t += e * x;
+        if (WITH_T) a.t += e * fmaxf(x, kLowest);
     };
     uint4 next[kStreamSlots];
     if (begin < end) {
@@ -1180,7 +1143,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
     }
     if (with_edge) {
         const int e = row.edge(tid);
-        const float z = e >= 0 ? Elem<T>::load(row.p + e) : 0.0f;
+        const float z = e >= 0 ? Elem<T>::load(row.p + e) : -INFINITY;
         if (z > a.m) rebase(z);
         if (e >= 0) add_one(z);
     }
@@ -1192,11 +1155,10 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
 #pragma unroll
             for (int k = 0; k < kStreamSlots; ++k) next[k] = row.load(min(i + STEP + k * 256, end - 1));
         }
-        uint32_t most = Elem<T>::kLeast;
+        uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
 #pragma unroll
-        for (int k = 0; k < kStreamSlots; ++k)
-            most = Elem<T>::more(Elem<T>::more(Elem<T>::more(Elem<T>::more(most, v[k].x), v[k].y), v[k].z), v[k].w);
-        const float m = Elem<T>::largest(most);
+        for (int k = 0; k < kStreamSlots; ++k) add_words<T>(v[k], most, least);
+        const float m = Elem<T>::largest(most, least);
         if (m > a.m) rebase(m);
 #pragma unroll
         for (int k = 0; k < kStreamSlots; ++k)
@@ -1207,22 +1169,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
                 for (int j = 0; j < N; ++j) add_one(f[j]);
             }
     }
-    a = merge_of<64>(a);
-    if (!(a.s >= 0x1p-100f) || a.t != a.t) {             // far below 0, -infinity among them, or not a number: once more, with care
-        a = Sums{};
-        if (with_edge) {
-            const int e = row.edge(tid);
-            const float f[1] = {e >= 0 ? Elem<T>::load(row.p + e) : -INFINITY};
-            add(a, f);
-        }
-        for (int i = begin + tid; i < end; i += 256) {
-            float f[N];
-            Elem<T>::unpack(row.load(i), f);
-            add(a, f);
-        }
-        a = merge_of<64>(a);
-    }
-    return a;
+    return merge_of<64>(a);
 }
 
 // PASS_LOGP and PASS_PREF_FORWARD of whole rows, or (slices > 1) the sums of the slices.

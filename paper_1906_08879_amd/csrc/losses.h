@@ -34,12 +34,12 @@ struct RowsView {
     bool all = true;                   // every row counts, known on the host
 };
 
-// Maximum m and sums over a slice of a row: of 2^x and of 2^x x, x = k z - o with k and o from m (ref_of).
+// Maximum m and sums over a slice of a row: of 2^x and of 2^x x, x = (z - m) log2 e.
 struct RowPart {
     float m, s, t;
 };
 
-// The gradient of a row: 2^x (A + B x) + C [j = a], x = k z_j - o with k and o from m (ref_of); all three zero: zeros.  Between the passes of a
+// The gradient of a row: 2^x (A + B x) + C [j = a], x = (z_j - m) log2 e; all three zero: zeros.  Between the passes of a
 // preference, A is 1 / s (0: the row adds nothing).
 struct RowGrad {
     float m, A, B, C;

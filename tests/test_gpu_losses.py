@@ -136,6 +136,36 @@ def test_values_at_the_ends_of_the_types(V, dtype):
         check_grad(_host(grad), dict(out, actions=a), np.abs(adv) + 1.0, dtype, "grad")
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", [1, 2, 8, 16, 40, 65, 500, 3000, 12345, 70001, 140001])
+def test_certain_actions_and_rows_below_zero(V, dtype):
+    """One action as good as certain: log probability and entropy 0 and no gradient, to the last bit.  Logits that are all
+    negative, near zero (log probabilities themselves) and far below it."""
+    import torch
+    import paper_1906_08879_amd as pl
+    rng = np.random.default_rng(V)
+    z, a = _state(rng, 6, V, dtype)
+    z[0] = -300.0; z[0, a[0]] = 37.3
+    z[1] = -np.inf; z[1, a[1]] = -41.7
+    z[2] -= np.log(np.exp(z[2] - z[2].max()).sum()) + z[2].max() + 1e-3
+    z[3] -= 60.0
+    z[4] = -1000.0 - np.abs(z[4])
+    z[5] = -0.0
+    z = torch.from_numpy(z).to(_t(dtype)).double().numpy()
+    x = _logits(z, dtype)
+    logp, ent, stats = torch.empty(6, device="cuda:0"), torch.empty(6, device="cuda:0"), torch.empty(5, device="cuda:0")
+    pl.action_logp(x, _dev(a), logp, ent)
+    _, l, H, _ = ol.softmax_rows(z, a)
+    check_rows(_host(logp), l, V, "logp")
+    check_rows(_host(ent), H, V, "entropy")
+    assert (_host(logp)[:2] == 0).all() and (_host(ent)[:2] == 0).all()
+    grad, adv = torch.full_like(x, 7.0), np.ones(6, np.float32)
+    pl.clipped_policy_loss(x, _dev(a), _dev(adv), stats, entropy_coeff=0.1, out_grad=grad)
+    out = ol.policy_loss(z, a, adv, entropy_coeff=0.1)
+    check_grad(_host(grad), dict(out, actions=a), adv + 1.0, dtype, "grad")
+    assert (_host(grad)[:2] == 0).all()
+
+
 def test_no_rows_and_masked_rows():
     import torch
     import paper_1906_08879_amd as pl
