@@ -194,6 +194,64 @@ __device__ __forceinline__ void store_slot(T *out, int e, int V, const float (&f
     }
 }
 
+// Rows of a few aligned bytes.
+template <int BYTES>
+struct Words {
+    static constexpr int N = BYTES / 4;
+    uint32_t w[N];
+    __device__ void load(const void *p)
+    {
+        if constexpr (BYTES == 4) w[0] = *static_cast<const uint32_t *>(p);
+        if constexpr (BYTES == 8) *this = from(*static_cast<const uint2 *>(p));
+        if constexpr (BYTES >= 16) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) {
+                const uint4 v = static_cast<const uint4 *>(p)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        }
+    }
+    __device__ void store(void *p) const
+    {
+        if constexpr (BYTES == 4) *static_cast<uint32_t *>(p) = w[0];
+        if constexpr (BYTES == 8) *static_cast<uint2 *>(p) = {w[0], w[1]};
+        if constexpr (BYTES >= 16) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) static_cast<uint4 *>(p)[i] = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+        }
+    }
+    static __device__ Words from(const uint2 &v)
+    {
+        Words r;
+        r.w[0] = v.x; r.w[1] = v.y;
+        return r;
+    }
+};
+
+template <typename T, int CAP>
+__device__ __forceinline__ void unpack_words(const uint32_t *w, float *f)
+{
+#pragma unroll
+    for (int j = 0; j < CAP; ++j) {
+        if constexpr (sizeof(T) == 4) f[j] = __uint_as_float(w[j]);
+        else f[j] = static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(w[j / 2] >> (16 * (j % 2)))));
+    }
+}
+
+template <typename T, int CAP>
+__device__ __forceinline__ void pack_words(const float *f, uint32_t *w)
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < CAP; ++j) w[j] = __float_as_uint(f[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < CAP; j += 2)
+            w[j / 2] = __builtin_bit_cast(uint16_t, static_cast<T>(f[j])) |
+                       static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<T>(f[j + 1]))) << 16;
+    }
+}
+
 template <typename F>
 void by_type(int dtype, F &&f)
 {

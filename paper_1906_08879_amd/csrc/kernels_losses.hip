@@ -827,6 +827,23 @@ __device__ __forceinline__ void finish_sums(const RowArgs &g, const double (*wav
     }
 }
 
+// The same from a part of every thread; sums[i]: sum i's.
+__device__ __forceinline__ void finish_block_sums(const RowArgs &g, double (*sums)[256])
+{
+    const int tid = threadIdx.x, i = tid >> 6, lane = tid & 63;      // wave i takes sum i
+    const double v = wave_sum((sums[i][lane] + sums[i][lane + 64]) + (sums[i][lane + 128] + sums[i][lane + 192]));
+    if (gridDim.x > 1) {
+        if (lane == 0) g.sums[static_cast<size_t>(blockIdx.x) * 4 + i] = v;
+    } else {
+        if (lane == 0) sums[i][0] = v;
+        __syncthreads();
+        if (tid == 0) {
+            const double all[4] = {sums[0][0], sums[1][0], sums[2][0], sums[3][0]};
+            policy_stats_out(all, g.policy.ref_logp ? g.policy.kl_coeff : 0.0f, g.policy.entropy_coeff, g.out_stats);
+        }
+    }
+}
+
 // ---- narrow rows (up to kNarrow actions): a row per thread, 256 rows through LDS, everything in one pass.
 // The rows' elements go in and out in the order they lie in memory, whatever their number; rows are an odd number
 // of words apart in LDS, so that the lanes' walks along their rows meet 32 different banks.
@@ -871,16 +888,14 @@ __device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, in
     }
 }
 
-// CAP > 0: the thread keeps its row in CAP registers.  WHOLE: rows of CAP actions are whole slots of 16 aligned bytes, which
-// the thread reads and writes itself, without LDS (rows of 8 floats, 800k of them: this, against CAP = 16 through LDS,
-// is what the last step of launch_rows measured).
+// CAP > 0: the thread keeps its row in CAP registers.  WHOLE: rows of CAP actions are 4, 8, 16 or 32 aligned bytes, which
+// the thread reads and writes itself, without LDS.
 template <typename T, int PASS, int CAP, bool WHOLE>
 __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
 {
-    constexpr int N = Elem<T>::N;
     constexpr bool kGrad = PASS == PASS_POLICY || PASS == PASS_PREF_GRAD;
     extern __shared__ float tile[];
-    __shared__ double sums[4][PASS == PASS_POLICY ? 256 : 1];
+    __shared__ double sums[PASS == PASS_POLICY ? 4 : 1][256];
     const int V = WHOLE ? CAP : g.x.V, pitch = V | 1, tid = threadIdx.x;
     const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 256, n = n0 + tid;
     const int count = static_cast<int>(min(int64_t{256}, g.x.n - n0));
@@ -900,20 +915,23 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
 #pragma unroll
             for (int j = 0; j < CAP; ++j)
                 if (WHOLE || j < V) f(j, reg[j]);
-        } else {
-            for (int j = 0; j < V; ++j) f(j, z[j]);
+        } else {                                         // eight at a time, their LDS reads together
+            int j = 0;
+            for (; j + 8 <= V; j += 8) {
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = z[j + k];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f(j + k, v[k]);
+            }
+            for (; j < V; ++j) f(j, z[j]);
         }
     };
     if (WHOLE) {
         if (in.p.counts) {
-            const uint4 *at = reinterpret_cast<const uint4 *>(static_cast<const T *>(g.x.data) + n * g.x.stride);
-#pragma unroll
-            for (int i = 0; i < CAP / N; ++i) {
-                float f[N];
-                Elem<T>::unpack(at[i], f);
-#pragma unroll
-                for (int j = 0; j < N; ++j) reg[i * N + j] = f[j];
-            }
+            Words<CAP * sizeof(T)> words;
+            words.load(static_cast<const T *>(g.x.data) + n * g.x.stride);
+            unpack_words<T, CAP>(words.w, reg);
         }
     } else {
         narrow_tile<T, false>(g.x.data, g.x.stride, n0, count, V, g.magic, pitch, tile);
@@ -945,14 +963,12 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
                 return none ? 0.0f : f[0] + (j == in.act ? rg.C : 0.0f);
             };
             if (WHOLE) {
-                T *out = static_cast<T *>(g.out_grad) + n * g.grad_stride;
+                float f[CAP > 0 ? CAP : 1];
 #pragma unroll
-                for (int i = 0; i < CAP / N; ++i) {
-                    float f[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) f[j] = gradient(i * N + j, reg[i * N + j]);
-                    *reinterpret_cast<uint4 *>(out + i * N) = Elem<T>::pack(f);
-                }
+                for (int j = 0; j < CAP; ++j) f[j] = gradient(j, reg[j]);
+                Words<CAP * sizeof(T)> words;
+                pack_words<T, CAP>(f, words.w);
+                words.store(static_cast<T *>(g.out_grad) + n * g.grad_stride);
             } else {
                 each([&](int j, float v) { z[j] = gradient(j, v); });
             }
@@ -965,18 +981,7 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
     if (PASS == PASS_POLICY) {
         for (int i = 0; i < 4; ++i) sums[i][tid] = acc[i];
         __syncthreads();
-        const int i = tid >> 6, lane = tid & 63;         // wave i takes sum i
-        const double v = wave_sum((sums[i][lane] + sums[i][lane + 64]) + (sums[i][lane + 128] + sums[i][lane + 192]));
-        if (gridDim.x > 1) {
-            if (lane == 0) g.sums[static_cast<size_t>(blockIdx.x) * 4 + i] = v;
-        } else {                                         // nobody else has sums
-            if (lane == 0) sums[i][0] = v;
-            __syncthreads();
-            if (tid == 0) {
-                const double all[4] = {sums[0][0], sums[1][0], sums[2][0], sums[3][0]};
-                policy_stats_out(all, g.policy.ref_logp ? g.policy.kl_coeff : 0.0f, g.policy.entropy_coeff, g.out_stats);
-            }
-        }
+        finish_block_sums(g, sums);
     }
 }
 
@@ -990,6 +995,135 @@ __device__ __forceinline__ void add_words(const uint4 &v, uint32_t &most, uint32
 
 // The slot stays in its four registers: without this the compiler keeps every unpacked value from one use to the next.
 __device__ __forceinline__ void keep_packed(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+
+// ---- rows of middling width: LANES lanes to a row, R rows of a lane one behind another, all of them in its registers; what
+// follows from the sums of the workgroup's rows is done a row to a thread, as for narrow rows: with a wave to a row it
+// took most of the time (131072 rows of 256 floats: 122 us).
+template <typename T, int LANES, int CH, int R, int PASS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k_group(RowArgs g)
+{
+    constexpr int N = Elem<T>::N, ABREAST = 256 / LANES, ROWS = ABREAST * R;
+    constexpr bool kGrad = PASS == PASS_POLICY || PASS == PASS_PREF_GRAD;
+    static_assert(ROWS <= 256 && LANES >= 2 * N, "a thread to a row, a lane to an element at an edge");
+    __shared__ RowPart part[ROWS];
+    __shared__ RowGrad grads[ROWS];
+    __shared__ int acts[ROWS];
+    __shared__ bool counts[ROWS];
+    __shared__ double sums[PASS == PASS_POLICY ? 4 : 1][256];
+    const int tid = threadIdx.x, lane = tid & (LANES - 1), V = g.x.V;
+    const int mine = LANES == 64 ? __builtin_amdgcn_readfirstlane(tid >> 6) : tid / LANES;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * ROWS;
+    const int rows = static_cast<int>(min(int64_t{ROWS}, g.x.n - n0));
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    RowIn in;
+    in.p.counts = false;
+    float z_a = 0.0f;
+    if (tid < rows) {
+        in.p = place_of(g.rows, n0 + tid);
+        if (in.p.counts) in.act = g.actions[n0 + tid];
+        read_in<PASS>(g, n0 + tid, in);
+        if (in.act >= 0 && in.act < V) z_a = Elem<T>::load(static_cast<const T *>(g.x.data) + (n0 + tid) * g.x.stride + in.act);
+        counts[tid] = in.p.counts;
+        if (kGrad) acts[tid] = in.act;
+    }
+    __syncthreads();
+    uint4 v[R * CH];
+    float z_edge[R];
+    auto span_of = [&](int r) { return Span<T>(static_cast<const T *>(g.x.data) + (n0 + r) * g.x.stride, V); };
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = i * ABREAST + mine;
+        z_edge[i] = -INFINITY;
+        if (r < rows && counts[r]) {
+            const Span<T> row = span_of(r);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) v[i * CH + k] = row.load(k * LANES + lane);
+            const int e = row.edge(lane);
+            if (e >= 0) z_edge[i] = Elem<T>::load(row.p + e);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = i * ABREAST + mine;
+        if (r < rows && counts[r]) {
+            const int whole = span_of(r).whole;
+            Sums a;
+            uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) add_words<T>(v[i * CH + k], most, least);
+            a.m = max_of<LANES>(fmaxf(z_edge[i], Elem<T>::largest(most, least)));
+            const Ref ref = ref_of(a.m);
+            auto add_one = [&](float z) {
+                const float x = ref(z), e = exp2_of(x);
+                a.s += e;
+                if (PASS == PASS_POLICY || PASS == PASS_LOGP) a.t += e * fmaxf(x, kLowest);
+            };
+            add_one(z_edge[i]);                          // (-infinity where there is none)
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (k * LANES + lane < whole) {
+                    float f[N];
+                    Elem<T>::unpack(v[i * CH + k], f);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) add_one(f[j]);
+                }
+            a.s = sum_of<LANES>(a.s);
+            if (PASS == PASS_POLICY || PASS == PASS_LOGP) a.t = sum_of<LANES>(a.t);
+            if (lane == 0) part[r] = {a.m, a.s, a.t};
+        }
+        if (kGrad) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) keep_packed(v[i * CH + k]);
+        }
+    }
+    __syncthreads();
+    if (tid < rows) {
+        const RowPart of = part[tid];
+        grads[tid] = finish_pass<PASS>(g, n0 + tid, in, in.p.counts ? Sums{of.m, of.s, of.t} : Sums{}, z_a, true, acc);
+    }
+    if (PASS == PASS_POLICY) {
+        for (int i = 0; i < 4; ++i) sums[i][tid] = acc[i];
+    }
+    __syncthreads();
+    if (kGrad && g.out_grad) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int r = i * ABREAST + mine;
+            if (r >= rows) continue;
+            const RowGrad rg = grads[r];
+            const Ref ref = ref_of(rg.m);
+            const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
+            const Span<T> row = span_of(r);
+            const int act = none ? -1 : acts[r], edge = row.edge(lane);
+            T *o = static_cast<T *>(g.out_grad) + (n0 + r) * g.grad_stride;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                const int slot = k * LANES + lane, e = row.head + slot * N;
+                if (slot < row.whole) {
+                    float f[N];
+                    if (none) {
+#pragma unroll
+                        for (int j = 0; j < N; ++j) f[j] = 0.0f;
+                    } else {
+                        Elem<T>::unpack(v[i * CH + k], f);
+                        grad_slot<N>(f, rg, ref);
+                        if (act >= e && act < e + N) {
+#pragma unroll
+                            for (int j = 0; j < N; ++j) f[j] += e + j == act ? rg.C : 0.0f;
+                        }
+                    }
+                    store_16(o + e, Elem<T>::pack(f));
+                }
+            }
+            if (edge >= 0) {
+                float f[1] = {z_edge[i]};
+                grad_slot<1>(f, rg, ref);
+                Elem<T>::store(o + edge, none ? 0.0f : f[0] + (edge == act ? rg.C : 0.0f));
+            }
+        }
+    }
+    if constexpr (PASS == PASS_POLICY) finish_block_sums(g, sums);
+}
 
 // ---- wider rows that fit in the registers of LANES threads: read once, the maximum and the sums of every wave, those of
 // the row in its first wave, the gradient from the registers.  Bound by memory: a pass that reads the row again for its
@@ -1210,6 +1344,11 @@ __global__ __launch_bounds__(256) void k_stream(RowArgs g, RowPart *__restrict__
     }
 }
 
+// Slots of 16 bytes in a row; those of the rows that k_narrow and k_group take, and the rows of a workgroup of k_group.
+constexpr int kGroupSlots = 256;
+int row_slots(const LogitsView &x) { return x.V / (x.dtype == PL_F32 ? 4 : 8); }
+int group_rows(int slots) { return slots <= 16 ? 256 : slots <= 32 ? 128 : slots <= 64 ? 64 : slots <= 128 ? 32 : 16; }
+
 bool few_rows(const LogitsView &x) { return x.n < 64 && x.V >= 16384; }
 
 int row_blocks(int64_t n) { return static_cast<int>((n + kRowsPerBlock - 1) / kRowsPerBlock); }
@@ -1295,7 +1434,7 @@ RowArgs row_args(const LogitsView &x, const RowsView &rows, const int32_t *actio
     return g;
 }
 
-// Whole rows in one pass (k_narrow, k_rows), and how many workgroups take them; 0 where they do not fit or where there are
+// Whole rows in one pass (k_narrow, k_group, k_rows), and how many workgroups take them; 0 where they do not fit or where there are
 // so few of them that a row is better cut into slices.
 template <int PASS>
 int launch_rows(const RowArgs &g, hipStream_t s)
@@ -1304,30 +1443,41 @@ int launch_rows(const RowArgs &g, hipStream_t s)
     by_type(g.x.dtype, [&](auto t) {
         using T = decltype(t);
         const int slots = g.x.V / Elem<T>::N;    // whole ones, at most
-        auto go = [&](auto kernel, int rows, int threads, size_t lds, int most) {
-            blocks = static_cast<int>(std::min<int64_t>((g.x.n + rows - 1) / rows, most));
+        auto launch = [&](auto kernel, int64_t grid, int threads, size_t lds) {
+            blocks = static_cast<int>(grid);
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, g);
         };
+        // kernels whose workgroups take `rows` rows each, and kernels whose workgroups go over the rows
+        auto go = [&](auto kernel, int rows, size_t lds = 0) { launch(kernel, (g.x.n + rows - 1) / rows, 256, lds); };
+        auto go_over = [&](auto kernel, int rows, int threads) {
+            launch(kernel, std::min<int64_t>((g.x.n + rows - 1) / rows, kMaxSumBlocks), threads, 0);
+        };
         if (g.x.V <= kNarrow) {
-            constexpr int N = Elem<T>::N;
-            const bool at_16 = (reinterpret_cast<uintptr_t>(g.x.data) | reinterpret_cast<uintptr_t>(g.out_grad)) % 16 == 0 &&
-                               g.x.stride % N == 0 && (!g.out_grad || g.grad_stride % N == 0);
+            constexpr int W = 4 / sizeof(T);             // elements of a word
+            const size_t bytes = g.x.V * sizeof(T), align = std::min<size_t>(bytes, 16);
+            const bool whole = (reinterpret_cast<uintptr_t>(g.x.data) | reinterpret_cast<uintptr_t>(g.out_grad)) % align == 0 &&
+                               g.x.stride * sizeof(T) % align == 0 && (!g.out_grad || g.grad_stride * sizeof(T) % align == 0);
             const size_t lds = 256 * (g.x.V | 1) * sizeof(float);
-            if (at_16 && g.x.V == N) go(k_narrow<T, PASS, N, true>, 256, 256, 0, 1 << 23);
-            else if (at_16 && g.x.V == 2 * N) go(k_narrow<T, PASS, 2 * N, true>, 256, 256, 0, 1 << 23);
-            else if (g.x.V <= 16) go(k_narrow<T, PASS, 16, false>, 256, 256, lds, 1 << 23);
-            else go(k_narrow<T, PASS, 0, false>, 256, 256, lds, 1 << 23);
+            if (whole && bytes == 4 && sizeof(T) == 2) go(k_narrow<T, PASS, 2, true>, 256);
+            else if (whole && bytes == 8) go(k_narrow<T, PASS, 2 * W, true>, 256);
+            else if (whole && bytes == 16) go(k_narrow<T, PASS, 4 * W, true>, 256);
+            else if (whole && bytes == 32) go(k_narrow<T, PASS, 8 * W, true>, 256);
+            else if (g.x.V <= 16) go(k_narrow<T, PASS, 16, false>, 256, lds);
+            else go(k_narrow<T, PASS, 0, false>, 256, lds);
         }
+        else if (slots <= 16) go(k_group<T, 16, 1, 16, PASS>, group_rows(slots));
+        else if (slots <= 32) go(k_group<T, 16, 2, 8, PASS>, group_rows(slots));
+        else if (slots <= 64) go(k_group<T, 64, 1, 16, PASS>, group_rows(slots));
+        else if (slots <= 128) go(k_group<T, 64, 2, 8, PASS>, group_rows(slots));
+        else if (slots <= 256) go(k_group<T, 64, 4, 4, PASS>, group_rows(slots));
         if constexpr (PASS == PASS_PREF_GRAD) return;
-        else if (g.x.V <= kNarrow) return;
-        else if (slots <= 16 * 2) go(k_rows<T, 16, 2, PASS>, 16, 256, 0, kMaxSumBlocks);
-        else if (slots <= 64 * 4) go(k_rows<T, 64, 4, PASS>, 4, 256, 0, kMaxSumBlocks);
-        else if (slots <= 64 * 16) go(k_rows<T, 64, 16, PASS>, 4, 256, 0, kMaxSumBlocks);
+        else if (slots <= kGroupSlots) return;
+        else if (slots <= 64 * 16) go_over(k_rows<T, 64, 16, PASS>, 4, 256);
         else if (few_rows(g.x)) return;
         else if constexpr (PASS == PASS_POLICY) {
-            if (slots <= 256 * 16) go(k_rows<T, 256, 16, PASS>, 1, 256, 0, kMaxSumBlocks);
-            else if (slots <= 512 * 16) go(k_rows<T, 512, 16, PASS>, 1, 512, 0, kMaxSumBlocks);
-            else if (slots <= 1024 * 16) go(k_rows<T, 1024, 16, PASS>, 1, 1024, 0, kMaxSumBlocks);
+            if (slots <= 256 * 16) go_over(k_rows<T, 256, 16, PASS>, 1, 256);
+            else if (slots <= 512 * 16) go_over(k_rows<T, 512, 16, PASS>, 1, 512);
+            else if (slots <= 1024 * 16) go_over(k_rows<T, 1024, 16, PASS>, 1, 1024);
         } else {
             blocks = static_cast<int>(std::min<int64_t>(g.x.n, 1 << 22));
             hipLaunchKernelGGL((k_stream<T, PASS>), dim3(blocks), dim3(256), 0, s, g, nullptr, 1, g.out_entropy != nullptr);
@@ -1365,7 +1515,9 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
     take(w.seq_coeff, S);
     take(w.weights, S);
     take(w.weight, 1);
-    take(w.sums, static_cast<size_t>(std::max(row_blocks(x.n), kMaxSumBlocks)) * 4);
+    const int slots = row_slots(x);
+    const int64_t sum_blocks = slots <= kGroupSlots ? (x.n + group_rows(slots) - 1) / group_rows(slots) : row_blocks(x.n);
+    take(w.sums, static_cast<size_t>(std::max<int64_t>(sum_blocks, kMaxSumBlocks)) * 4);
     w.bytes = pos;
     return w;
 }
@@ -1433,7 +1585,7 @@ void launch_preference_loss(const LogitsView &x, const RowsView &rows, const Pre
     g.logp = ws.logp;
     g.grad = ws.grad;
     // rows that are read fast again whole need nothing kept of them
-    const bool again = x.V <= kNarrow;
+    const bool again = row_slots(x) <= kGroupSlots;
     if (again) g.grad = nullptr;
     if (x.n > 0 && !launch_rows<PASS_PREF_FORWARD>(g, s)) {
         launch_parts(g, ws, false, s);

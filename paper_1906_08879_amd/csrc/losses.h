@@ -77,7 +77,7 @@ struct LossWorkspace {
     float *seq_coeff = nullptr;        // [S]
     float *weights = nullptr;          // [S], for PL_REDUCE_SEQS
     float *weight = nullptr;           // [1], for PL_REDUCE_ROWS
-    double *sums = nullptr;            // [workgroups, 4]: kMaxSumBlocks, or one for kRowsPerBlock rows
+    double *sums = nullptr;            // [workgroups, 4]
     int slices = 1, seq_parts = 1;
     size_t bytes = 0;
 };
