@@ -170,15 +170,34 @@ struct Span {
     }
 };
 
-// 16 bytes to an address that is aligned to its elements only (one store instruction all the same, slower where a
+// 16 bytes to or from an address that is aligned to its elements only (one instruction all the same, slower where a
 // cache line ends within it).
 typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
 __device__ __forceinline__ void store_16(T *out, const uint4 &v)
 {
+    if (sizeof(T) == 4) *reinterpret_cast<words_at_4 *>(out) = words_at_4{v.x, v.y, v.z, v.w};
+    else *reinterpret_cast<words_at_2 *>(out) = words_at_2{v.x, v.y, v.z, v.w};
+}
+
+// The same past the caches, which keep what they hold: for whole cache lines of a stream that is not read again soon.
+template <typename T>
+__device__ __forceinline__ void stream_16(T *out, const uint4 &v)
+{
     if (sizeof(T) == 4) __builtin_nontemporal_store(words_at_4{v.x, v.y, v.z, v.w}, reinterpret_cast<words_at_4 *>(out));
     else __builtin_nontemporal_store(words_at_2{v.x, v.y, v.z, v.w}, reinterpret_cast<words_at_2 *>(out));
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 load_16(const T *in)
+{
+    if (sizeof(T) == 4) {
+        const words_at_4 v = *reinterpret_cast<const words_at_4 *>(in);
+        return {v.x, v.y, v.z, v.w};
+    }
+    const words_at_2 v = *reinterpret_cast<const words_at_2 *>(in);
+    return {v.x, v.y, v.z, v.w};
 }
 
 template <typename T>

@@ -131,7 +131,7 @@ __device__ __forceinline__ void chunk_scale(const ClipTable &t, const Chunk &c, 
                     for (int j = 0; j < N; ++j) f[j] = ldexpf(f[j] * by.m, by.e);
                     v[k] = Elem<T>::pack(f);
                 }
-                store_16(o + span.head + static_cast<uint32_t>(i + k * THREADS) * N, v[k]);
+                stream_16(o + span.head + static_cast<uint32_t>(i + k * THREADS) * N, v[k]);
             }
     }
     if (const int e = span.edge(threadIdx.x); e >= 0) {

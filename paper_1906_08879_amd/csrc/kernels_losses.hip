@@ -30,11 +30,23 @@ struct Ref {
 };
 __device__ __forceinline__ Ref ref_of(float m) { return {m == -INFINITY ? 0.0f : m}; }
 
-// ---- over 16 lanes (a DPP row) and over a wave
+// ---- over 4 lanes, 16 lanes (a DPP row) and a wave
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
+__device__ __forceinline__ float max_of_4(float v)
+{
+    v = fmaxf(v, dpp<0xb1>(v));        // within four lanes: the neighbour, then the other pair
+    return fmaxf(v, dpp<0x4e>(v));
+}
+
+__device__ __forceinline__ float sum_of_4(float v)
+{
+    v += dpp<0xb1>(v);
+    return v + dpp<0x4e>(v);
 }
 
 __device__ __forceinline__ float max_of_16(float v)
@@ -61,6 +73,7 @@ __device__ __forceinline__ float lane_value(float v, int lane)
 template <int LANES>
 __device__ __forceinline__ float max_of(float v)
 {
+    if (LANES == 4) return max_of_4(v);
     v = max_of_16(v);
     if (LANES == 16) return v;
     return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
@@ -69,6 +82,7 @@ __device__ __forceinline__ float max_of(float v)
 template <int LANES>
 __device__ __forceinline__ float sum_of(float v)
 {
+    if (LANES == 4) return sum_of_4(v);
     v = sum_of_16(v);
     if (LANES == 16) return v;
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
@@ -403,7 +417,7 @@ __global__ __launch_bounds__(256) void k_row_grad(GradArgs a)
                         for (int j = 0; j < N; ++j) f[j] += e + j == act ? g.C : 0.0f;
                     }
                 }
-                store_16(o + e, Elem<T>::pack(f));
+                stream_16(o + e, Elem<T>::pack(f));
             }
         }
         if (edge >= 0) {
@@ -888,7 +902,7 @@ __device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, in
     }
 }
 
-// CAP > 0: the thread keeps its row in CAP registers.  WHOLE: rows of CAP actions are 4, 8, 16 or 32 aligned bytes, which
+// The thread keeps its row in CAP registers.  WHOLE: rows of CAP actions are 4, 8, 16 or 32 aligned bytes, which
 // the thread reads and writes itself, without LDS.
 template <typename T, int PASS, int CAP, bool WHOLE>
 __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
@@ -907,25 +921,13 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
         if (in.p.counts) in.act = g.actions[n];
         read_in<PASS>(g, n, in);
     }
-    float reg[CAP > 0 ? CAP : 1];
+    float reg[CAP];
     float *z = tile + tid * pitch;
     // f(j, logit j) for every action
     auto each = [&](auto f) {
-        if (CAP > 0) {
 #pragma unroll
-            for (int j = 0; j < CAP; ++j)
-                if (WHOLE || j < V) f(j, reg[j]);
-        } else {                                         // eight at a time, their LDS reads together
-            int j = 0;
-            for (; j + 8 <= V; j += 8) {
-                float v[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = z[j + k];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) f(j + k, v[k]);
-            }
-            for (; j < V; ++j) f(j, z[j]);
-        }
+        for (int j = 0; j < CAP; ++j)
+            if (WHOLE || j < V) f(j, reg[j]);
     };
     if (WHOLE) {
         if (in.p.counts) {
@@ -963,7 +965,7 @@ __global__ __launch_bounds__(256) void k_narrow(RowArgs g)
                 return none ? 0.0f : f[0] + (j == in.act ? rg.C : 0.0f);
             };
             if (WHOLE) {
-                float f[CAP > 0 ? CAP : 1];
+                float f[CAP];
 #pragma unroll
                 for (int j = 0; j < CAP; ++j) f[j] = gradient(j, reg[j]);
                 Words<CAP * sizeof(T)> words;
@@ -998,13 +1000,18 @@ __device__ __forceinline__ void keep_packed(uint4 &v) { asm volatile("" : "+v"(v
 
 // ---- rows of middling width: LANES lanes to a row, R rows of a lane one behind another, all of them in its registers; what
 // follows from the sums of the workgroup's rows is done a row to a thread, as for narrow rows: with a wave to a row it
-// took most of the time (131072 rows of 256 floats: 122 us).
-template <typename T, int LANES, int CH, int R, int PASS>
+// took most of the time (131072 rows of 256 floats: 122 us, against 74).
+// A row is cut into slots of 16 bytes from its start, aligned or not; the last one is the row's last 16 bytes, some of which
+// the slot before has too: they are left out of the sums, and their gradient is written twice, the same.
+// STREAM: the gradient goes past the caches, where every row of it begins at a multiple of 16 bytes (65536 rows of 512
+// floats: 53 us against 64); lines that several stores fill in parts are better put together in them (671040 rows of 100
+// bf16: 167 us against 91).
+template <typename T, int LANES, int CH, int R, int PASS, bool STREAM>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k_group(RowArgs g)
 {
     constexpr int N = Elem<T>::N, ABREAST = 256 / LANES, ROWS = ABREAST * R;
     constexpr bool kGrad = PASS == PASS_POLICY || PASS == PASS_PREF_GRAD;
-    static_assert(ROWS <= 256 && LANES >= 2 * N, "a thread to a row, a lane to an element at an edge");
+    static_assert(ROWS <= 256, "a thread to a row");
     __shared__ RowPart part[ROWS];
     __shared__ RowGrad grads[ROWS];
     __shared__ int acts[ROWS];
@@ -1027,45 +1034,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
         if (kGrad) acts[tid] = in.act;
     }
     __syncthreads();
+    // first element of slot k of this lane; the elements of it that the slot before has
+    auto start = [&](int k) { return min((k * LANES + lane) * N, V - N); };
+    auto twice = [&](int k) { return (k * LANES + lane) * N - start(k); };
     uint4 v[R * CH];
-    float z_edge[R];
-    auto span_of = [&](int r) { return Span<T>(static_cast<const T *>(g.x.data) + (n0 + r) * g.x.stride, V); };
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int r = i * ABREAST + mine;
-        z_edge[i] = -INFINITY;
         if (r < rows && counts[r]) {
-            const Span<T> row = span_of(r);
+            const T *row = static_cast<const T *>(g.x.data) + (n0 + r) * g.x.stride;
 #pragma unroll
-            for (int k = 0; k < CH; ++k) v[i * CH + k] = row.load(k * LANES + lane);
-            const int e = row.edge(lane);
-            if (e >= 0) z_edge[i] = Elem<T>::load(row.p + e);
+            for (int k = 0; k < CH; ++k) v[i * CH + k] = load_16(row + start(k));
         }
     }
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int r = i * ABREAST + mine;
         if (r < rows && counts[r]) {
-            const int whole = span_of(r).whole;
             Sums a;
             uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
 #pragma unroll
             for (int k = 0; k < CH; ++k) add_words<T>(v[i * CH + k], most, least);
-            a.m = max_of<LANES>(fmaxf(z_edge[i], Elem<T>::largest(most, least)));
+            a.m = max_of<LANES>(Elem<T>::largest(most, least));
             const Ref ref = ref_of(a.m);
-            auto add_one = [&](float z) {
-                const float x = ref(z), e = exp2_of(x);
-                a.s += e;
-                if (PASS == PASS_POLICY || PASS == PASS_LOGP) a.t += e * fmaxf(x, kLowest);
-            };
-            add_one(z_edge[i]);                          // (-infinity where there is none)
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (k * LANES + lane < whole) {
+                if ((k * LANES + lane) * N < V) {
                     float f[N];
                     Elem<T>::unpack(v[i * CH + k], f);
+                    if (V % N) {
+                        const int skip = twice(k);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) add_one(f[j]);
+                        for (int j = 0; j < N; ++j) f[j] = j < skip ? -INFINITY : f[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float x = ref(f[j]), e = exp2_of(x);
+                        a.s += e;
+                        if (PASS == PASS_POLICY || PASS == PASS_LOGP) a.t += e * fmaxf(x, kLowest);
+                    }
                 }
             a.s = sum_of<LANES>(a.s);
             if (PASS == PASS_POLICY || PASS == PASS_LOGP) a.t = sum_of<LANES>(a.t);
@@ -1093,13 +1100,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
             const RowGrad rg = grads[r];
             const Ref ref = ref_of(rg.m);
             const bool none = rg.A == 0.0f && rg.B == 0.0f && rg.C == 0.0f;
-            const Span<T> row = span_of(r);
-            const int act = none ? -1 : acts[r], edge = row.edge(lane);
+            const int act = none ? -1 : acts[r];
             T *o = static_cast<T *>(g.out_grad) + (n0 + r) * g.grad_stride;
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int slot = k * LANES + lane, e = row.head + slot * N;
-                if (slot < row.whole) {
+            for (int k = 0; k < CH; ++k)
+                if ((k * LANES + lane) * N < V) {
+                    const int e = start(k);
                     float f[N];
                     if (none) {
 #pragma unroll
@@ -1112,14 +1118,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
                             for (int j = 0; j < N; ++j) f[j] += e + j == act ? rg.C : 0.0f;
                         }
                     }
-                    store_16(o + e, Elem<T>::pack(f));
+                    if (STREAM) stream_16(o + e, Elem<T>::pack(f));
+                    else store_16(o + e, Elem<T>::pack(f));
                 }
-            }
-            if (edge >= 0) {
-                float f[1] = {z_edge[i]};
-                grad_slot<1>(f, rg, ref);
-                Elem<T>::store(o + edge, none ? 0.0f : f[0] + (edge == act ? rg.C : 0.0f));
-            }
         }
     }
     if constexpr (PASS == PASS_POLICY) finish_block_sums(g, sums);
@@ -1225,7 +1226,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
                         Elem<T>::unpack(v[k], f);
                         grad_slot<N>(f, rg, ref);
                     }
-                    store_16(o + head + static_cast<uint32_t>(k * LANES + lane) * N, Elem<T>::pack(f));
+                    stream_16(o + head + static_cast<uint32_t>(k * LANES + lane) * N, Elem<T>::pack(f));
                 }
             }
             if (edge >= 0) {
@@ -1344,9 +1345,9 @@ __global__ __launch_bounds__(256) void k_stream(RowArgs g, RowPart *__restrict__
     }
 }
 
-// Slots of 16 bytes in a row; those of the rows that k_narrow and k_group take, and the rows of a workgroup of k_group.
+// Slots of 16 bytes in a row, the last one begun; those of the rows that k_narrow and k_group take, and the rows of a workgroup of k_group.
 constexpr int kGroupSlots = 256;
-int row_slots(const LogitsView &x) { return x.V / (x.dtype == PL_F32 ? 4 : 8); }
+int row_slots(const LogitsView &x) { return x.dtype == PL_F32 ? (x.V + 3) / 4 : (x.V + 7) / 8; }
 int group_rows(int slots) { return slots <= 16 ? 256 : slots <= 32 ? 128 : slots <= 64 ? 64 : slots <= 128 ? 32 : 16; }
 
 bool few_rows(const LogitsView &x) { return x.n < 64 && x.V >= 16384; }
@@ -1440,9 +1441,10 @@ template <int PASS>
 int launch_rows(const RowArgs &g, hipStream_t s)
 {
     int blocks = 0;
+
     by_type(g.x.dtype, [&](auto t) {
         using T = decltype(t);
-        const int slots = g.x.V / Elem<T>::N;    // whole ones, at most
+        const int slots = row_slots(g.x), whole_slots = g.x.V / Elem<T>::N;
         auto launch = [&](auto kernel, int64_t grid, int threads, size_t lds) {
             blocks = static_cast<int>(grid);
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, g);
@@ -1451,6 +1453,13 @@ int launch_rows(const RowArgs &g, hipStream_t s)
         auto go = [&](auto kernel, int rows, size_t lds = 0) { launch(kernel, (g.x.n + rows - 1) / rows, 256, lds); };
         auto go_over = [&](auto kernel, int rows, int threads) {
             launch(kernel, std::min<int64_t>((g.x.n + rows - 1) / rows, kMaxSumBlocks), threads, 0);
+        };
+        auto group = [&](auto f) {
+            if constexpr (PASS == PASS_POLICY || PASS == PASS_PREF_GRAD) {
+                const bool at_16 = reinterpret_cast<uintptr_t>(g.out_grad) % 16 == 0 && g.grad_stride * sizeof(T) % 16 == 0;
+                if (at_16) return f(std::true_type{});
+            }
+            f(std::false_type{});
         };
         if (g.x.V <= kNarrow) {
             constexpr int W = 4 / sizeof(T);             // elements of a word
@@ -1462,22 +1471,23 @@ int launch_rows(const RowArgs &g, hipStream_t s)
             else if (whole && bytes == 8) go(k_narrow<T, PASS, 2 * W, true>, 256);
             else if (whole && bytes == 16) go(k_narrow<T, PASS, 4 * W, true>, 256);
             else if (whole && bytes == 32) go(k_narrow<T, PASS, 8 * W, true>, 256);
-            else if (g.x.V <= 16) go(k_narrow<T, PASS, 16, false>, 256, lds);
-            else go(k_narrow<T, PASS, 0, false>, 256, lds);
+            else go(k_narrow<T, PASS, kNarrow, false>, 256, lds);
         }
-        else if (slots <= 16) go(k_group<T, 16, 1, 16, PASS>, group_rows(slots));
-        else if (slots <= 32) go(k_group<T, 16, 2, 8, PASS>, group_rows(slots));
-        else if (slots <= 64) go(k_group<T, 64, 1, 16, PASS>, group_rows(slots));
-        else if (slots <= 128) go(k_group<T, 64, 2, 8, PASS>, group_rows(slots));
-        else if (slots <= 256) go(k_group<T, 64, 4, 4, PASS>, group_rows(slots));
+        else if (slots <= 4) group([&](auto stream) { go(k_group<T, 4, 1, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
+        else if (slots <= 8) group([&](auto stream) { go(k_group<T, 4, 2, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
+        else if (slots <= 16) group([&](auto stream) { go(k_group<T, 4, 4, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
+        else if (slots <= 32) group([&](auto stream) { go(k_group<T, 16, 2, 8, PASS, decltype(stream)::value>, group_rows(slots)); });
+        else if (slots <= 64) group([&](auto stream) { go(k_group<T, 16, 4, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
+        else if (slots <= 128) group([&](auto stream) { go(k_group<T, 16, 8, 2, PASS, decltype(stream)::value>, group_rows(slots)); });
+        else if (slots <= 256) group([&](auto stream) { go(k_group<T, 64, 4, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
         if constexpr (PASS == PASS_PREF_GRAD) return;
         else if (slots <= kGroupSlots) return;
-        else if (slots <= 64 * 16) go_over(k_rows<T, 64, 16, PASS>, 4, 256);
+        else if (whole_slots <= 64 * 16) go_over(k_rows<T, 64, 16, PASS>, 4, 256);
         else if (few_rows(g.x)) return;
         else if constexpr (PASS == PASS_POLICY) {
-            if (slots <= 256 * 16) go_over(k_rows<T, 256, 16, PASS>, 1, 256);
-            else if (slots <= 512 * 16) go_over(k_rows<T, 512, 16, PASS>, 1, 512);
-            else if (slots <= 1024 * 16) go_over(k_rows<T, 1024, 16, PASS>, 1, 1024);
+            if (whole_slots <= 256 * 16) go_over(k_rows<T, 256, 16, PASS>, 1, 256);
+            else if (whole_slots <= 512 * 16) go_over(k_rows<T, 512, 16, PASS>, 1, 512);
+            else if (whole_slots <= 1024 * 16) go_over(k_rows<T, 1024, 16, PASS>, 1, 1024);
         } else {
             blocks = static_cast<int>(std::min<int64_t>(g.x.n, 1 << 22));
             hipLaunchKernelGGL((k_stream<T, PASS>), dim3(blocks), dim3(256), 0, s, g, nullptr, 1, g.out_entropy != nullptr);

@@ -9,7 +9,7 @@
 namespace pl {
 
 constexpr int kMaxActions = 1 << 24;
-constexpr int kNarrow = 64;            // actions of rows that a thread takes
+constexpr int kNarrow = 16;            // actions of rows that a thread takes
 constexpr int kMaxSlices = 64;         // parts that a row is cut into where there are few rows
 constexpr int kRowsPerBlock = 256;     // rows of a workgroup of the per-row kernels
 constexpr int kMiddleRows = 32768;     // rows, and sequences, whose sums and pairs one workgroup does
