@@ -170,12 +170,12 @@ int pl_preference_loss(const pl_logits *logits, const pl_rows *rows_in, const pl
     return PL_OK;
 }
 
-// Sums of every launch's workgroups.
+// Sums of the workgroups, and the list of the tensors where they do not go by value.
 size_t pl_clip_gradients_workspace(int32_t n_tensors)
 {
     if (n_tensors < 0) return 0;
-    const size_t launches = (static_cast<size_t>(n_tensors) + kClipTensors - 1) / kClipTensors;
-    return std::max<size_t>(1, launches) * kClipBlocks * sizeof(double);
+    const size_t n = static_cast<size_t>(n_tensors), list = n > kClipTensors ? n * sizeof(ClipTensor) + (n + 1) * sizeof(int32_t) : 0;
+    return kClipBlocks * sizeof(double) + (list + 15) / 16 * 16;
 }
 
 int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clipped, const int64_t *numel,
@@ -205,47 +205,46 @@ int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clippe
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     double *sums = static_cast<double *>(workspace);
-    const size_t launches = (static_cast<size_t>(n_tensors) + kClipTensors - 1) / kClipTensors;
-    // every launch's tensors, without the empty ones; chunks as small as a workgroup's loads for a thread, as long as
-    // there are fewer of them than workgroups
-    // (a workgroup that does all alone takes a tensor at a time)
+    // chunks of eight slots to a thread, as long as there are fewer of them than workgroups; a workgroup that does all alone
+    // takes a tensor at a time
     const bool small = n_tensors <= 4 && total <= kClipSmall;
-    const int chunk = small ? static_cast<int>(kClipSmall) : static_cast<int>(std::min<int64_t>(kClipChunk, std::max<int64_t>(2048, total / kClipBlocks / 2048 * 2048)));
-    auto table = [&](size_t launch) {
+    const int chunk = static_cast<int>(small ? kClipSmall : std::min<int64_t>(kClipChunk, std::max<int64_t>(2048, total / kClipBlocks / 2048 * 2048)));
+    // tables of the tensors, without the empty ones
+    int32_t next = 0;
+    int64_t chunks = 0;
+    auto table = [&]() {
         ClipTable t;
         t.n = 0;
         t.chunk = chunk;
-        t.first[0] = 0;
-        const size_t end = std::min<size_t>(n_tensors, (launch + 1) * kClipTensors);
-        for (size_t i = launch * kClipTensors; i < end; ++i) {
-            if (numel[i] == 0) continue;
-            t.src[t.n] = grads[i];
-            t.dst[t.n] = clipped ? clipped[i] : grads[i];
-            t.numel[t.n] = numel[i];
-            t.dtype[t.n] = static_cast<uint8_t>(dtype[i]);
-            t.first[t.n + 1] = t.first[t.n] + static_cast<int32_t>((numel[i] + chunk - 1) / chunk);
-            ++t.n;
+        t.first[0] = static_cast<int32_t>(chunks);
+        for (; next < n_tensors && t.n < kClipTensors; ++next) {
+            if (numel[next] == 0) continue;
+            t.src[t.n] = grads[next];
+            t.dst[t.n] = clipped ? clipped[next] : grads[next];
+            t.numel[t.n] = numel[next];
+            t.dtype[t.n] = static_cast<uint8_t>(dtype[next]);
+            chunks += (numel[next] + chunk - 1) / chunk;
+            t.first[++t.n] = static_cast<int32_t>(chunks);
         }
         return t;
     };
-    if (small) {
-        launch_clip_small(table(0), max_norm, out_norm, s);
+    ClipTable t = table();
+    if (next == n_tensors) {
+        if (small) launch_clip_small(t, max_norm, out_norm, s);
+        else launch_clip(t, chunks, sums, max_norm, scales, out_norm, s);
     } else {
-        int n_sums = 0;
-        for (size_t l = 0; l < launches; ++l) {
-            const ClipTable t = table(l);
-            launch_clip_sums(t, sums + n_sums, s);
-            n_sums += clip_blocks(t);
+        ClipList list;
+        list.tensors = reinterpret_cast<ClipTensor *>(sums + kClipBlocks);
+        list.first = reinterpret_cast<int32_t *>(list.tensors + n_tensors);
+        list.n = 0;
+        list.chunk = chunk;
+        for (;; t = table()) {
+            launch_clip_list(t, list, list.n, s);
+            list.n += t.n;
+            if (next == n_tensors) break;
         }
-        if (!scales) launch_clip_norm(sums, n_sums, out_norm, s);
-        bool first = true;                       // the norm is written by the first launch that has tensors
-        for (size_t l = launches; scales && l-- > 0;) {
-            const ClipTable t = table(l);
-            launch_clip_scale(t, sums, n_sums, max_norm, first ? out_norm : nullptr, s);
-            first = first && !clip_blocks(t);
-        }
-        // (tensors without elements alone: launches, but none of them has a workgroup)
-        if (scales && first) launch_clip_norm(sums, n_sums, out_norm, s);
+        list.chunks = static_cast<int32_t>(chunks);
+        launch_clip(list, chunks, sums, max_norm, scales, out_norm, s);
     }
     PL_HIP(hipGetLastError());
     return PL_OK;

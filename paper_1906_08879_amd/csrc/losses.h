@@ -92,9 +92,19 @@ void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyA
 void launch_preference_loss(const LogitsView &x, const RowsView &rows, const PrefArgs &a, float *out_stats, void *out_grad,
                             int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
 
-// csrc/kernels_clip.hip: tensors of one launch, passed by value (a kernel's arguments end at 4 KiB)
+// csrc/kernels_clip.hip: the tensors of a call in chunks.  Up to kClipTensors of them go to the kernels by value (a kernel's
+// arguments end at 4 KiB), more through a list in the workspace that is written from such tables.
 constexpr int kClipTensors = 128;
-constexpr int kClipBlocks = 1024;
+constexpr int kClipBlocks = 1024;      // workgroups, and partial sums, at most
+constexpr int kClipChunk = 16384;      // elements of a chunk, at most
+constexpr int64_t kClipSmall = 32768;  // elements of a call that one workgroup does alone
+
+struct ClipTensor {
+    const void *src;
+    void *dst;
+    int64_t numel;
+    int64_t dtype;
+};
 struct ClipTable {
     const void *src[kClipTensors];
     void *dst[kClipTensors];
@@ -103,14 +113,17 @@ struct ClipTable {
     uint8_t dtype[kClipTensors];
     int32_t n, chunk;                  // tensors; elements of a chunk
 };
-constexpr int kClipChunk = 16384;      // the most elements of a chunk
-constexpr int64_t kClipSmall = 32768;  // elements of a call that one workgroup does alone
+struct ClipList {
+    ClipTensor *tensors;
+    int32_t *first;                    // [n + 1]
+    int32_t n, chunk, chunks;
+};
 
-int clip_blocks(const ClipTable &t);   // workgroups, and partial sums, of a launch
-void launch_clip_sums(const ClipTable &t, double *sums, hipStream_t s);
-void launch_clip_norm(const double *sums, int n_sums, float *out_norm, hipStream_t s);
-// (writes out_norm, if given, as well)
-void launch_clip_scale(const ClipTable &t, const double *sums, int n_sums, float max_norm, float *out_norm, hipStream_t s);
+int clip_blocks(int64_t chunks);       // workgroups, and partial sums, of a launch
+// The tensors of a table, from number `at` of the list on; the last call's table ends the list.
+void launch_clip_list(const ClipTable &t, const ClipList &list, int at, hipStream_t s);
+template <typename Tensors>            // ClipTable or ClipList
+void launch_clip(const Tensors &t, int64_t chunks, double *sums, float max_norm, bool scales, float *out_norm, hipStream_t s);
 void launch_clip_small(const ClipTable &t, float max_norm, float *out_norm, hipStream_t s);
 
 }  // namespace pl
