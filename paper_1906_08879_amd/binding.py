@@ -60,7 +60,7 @@ def library_path() -> str:
 def load_library(path: Optional[str] = None):
     """Load libplaceto.so and declare every signature of include/placeto.h."""
     global _lib
-    if _lib is not None and path is None:
+    if path is None and _lib is not None:
         return _lib
     path = path or _LIB_PATH
     if not os.path.exists(path):
@@ -143,26 +143,34 @@ def _i32(a):
 
 def _dev_ptr(t, dtype, n_min, name):
     """Pointer of a contiguous torch tensor living on a HIP device."""
-    import torch
     if t is None:
         return None
+    try:
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() >= n_min:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise PlacetoError(f"{name} must be a device tensor")
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n_min:
-        raise PlacetoError(f"{name}: expected contiguous {dtype} with >= {n_min} elements, "
-                           f"got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr()
+    raise PlacetoError(f"{name}: expected contiguous {dtype} with >= {n_min} elements, "
+                       f"got {t.dtype} {tuple(t.shape)}")
+
+
+_current_stream = None                  # handle of the current stream, without the Stream object around it
 
 
 def _stream_ptr(stream):
-    import torch
+    global _current_stream
     if stream is not None:
         return stream.cuda_stream
-    # the current stream's handle without the Stream object around it, which costs as much as a kernel launch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None or not torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
+    if _current_stream is None:
+        import torch
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+        if raw is None or not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        _current_stream = lambda: raw(device())  # noqa: E731
+    return _current_stream()
 
 
 def weights_count(D, H, n_layers=2, k_sweeps=1, group_by_device=1, weight_dtype="fp32") -> int:
