@@ -379,7 +379,7 @@ int pl_simulate_reward_ex(pl_graph_batch *g, int32_t D, const float *node_feats,
  * Numbers: probabilities are taken in fp32 from logits of any type, sums over rows in float64;
  * gradients are rounded once to the logits' type.  Summation orders are fixed: equal inputs
  * give equal bits.  A logit of -inf (or of its type's lowest value beside larger ones) is an action
- * of probability zero.  Rows that do not count (pl_rows) are not read: whatever their logits,
+ * of probability zero.  Rows that do not count (pl_rows) are not used: whatever their logits,
  * actions or other entries hold, their outputs are zero.  A row that counts whose action is
  * outside [0, n_actions) or has probability zero adds nothing to a loss or a gradient (its
  * gradient is zero, its weight stays with the rows' number) and gets the log probability NaN
@@ -410,7 +410,7 @@ typedef struct {
  *   mask    dev [n_rows]: 0 = the row does not count; NULL = all do */
 enum { PL_ROWS_BY_SEQ = 0, PL_ROWS_BY_STEP = 1, PL_ROWS_PACKED = 2 };
 typedef struct {
-    int32_t n_seqs;         /* >= 1 (n_rows a multiple of it unless packed)                        */
+    int32_t n_seqs;         /* 1 .. 2^23 (n_rows a multiple of it unless packed)                   */
     int32_t order;
     const int32_t *bounds;
     const uint8_t *mask;

@@ -37,7 +37,7 @@ int view_rows(const pl_rows *in, const LogitsView &x, RowsView *r)
         return PL_OK;
     }
     if (in->order < PL_ROWS_BY_SEQ || in->order > PL_ROWS_PACKED) return fail(PL_ERR_SHAPE, "unknown order of rows");
-    if (in->n_seqs < 1 || in->n_seqs > (1 << 24)) return fail(PL_ERR_SHAPE, "n_seqs must be 1 .. 2^24");
+    if (in->n_seqs < 1 || in->n_seqs > (1 << 23)) return fail(PL_ERR_SHAPE, "n_seqs must be 1 .. 2^23");
     r->S = in->n_seqs;
     r->order = in->order;
     if (in->order == PL_ROWS_PACKED) {

@@ -184,43 +184,6 @@ __device__ __forceinline__ void finish_row(const Sums &a, float z_a, bool action
     if (a.s == 0.0f) H = l = NAN;
 }
 
-template <typename T>
-__device__ __forceinline__ float logit(const LogitsView &x, int64_t n, int a)
-{
-    return Elem<T>::load(static_cast<const T *>(x.data) + n * x.stride + a);
-}
-
-// ---- one row per thread: log probabilities, and what the gradient of a preference needs
-template <typename T>
-__global__ __launch_bounds__(kRowsPerBlock) void k_finish_logp(LogitsView x, RowsView rows, const int32_t *__restrict__ actions,
-                                                               const RowPart *__restrict__ parts, int slices,
-                                                               float *__restrict__ out_logp, float *__restrict__ out_entropy,
-                                                               double *__restrict__ logp, RowGrad *__restrict__ grad)
-{
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + threadIdx.x;
-    if (n >= x.n) return;
-    float l = 0.0f, H = 0.0f;
-    double exact = kAddsNothing;
-    RowGrad g{0.0f, 0.0f, 0.0f, 0.0f};
-    if (place_of(rows, n).counts) {
-        const Sums a = merged_parts(parts + n * slices, slices);
-        const int act = actions[n];
-        const bool ok = act >= 0 && act < x.V;
-        const float z_a = ok ? logit<T>(x, n, act) : 0.0f;
-        float log_s;
-        finish_row(a, z_a, ok, l, H, log_s);
-        g.m = a.m;
-        if (ok && l != -INFINITY && a.s != 0.0f) {
-            g.A = 1.0f / a.s;
-            exact = exact_l(a, z_a);
-        }
-    }
-    if (out_logp) out_logp[n] = l;
-    if (logp) logp[n] = exact;
-    if (out_entropy) out_entropy[n] = H;
-    if (grad) grad[n] = g;
-}
-
 struct PolicyRow {
     float c = 0.0f, g = 0.0f;          // - d loss / d l, - d loss / d H, without the gradient's scale
     float sur = 0.0f, kl = 0.0f, H = 0.0f, cut = 0.0f;
@@ -269,52 +232,6 @@ __device__ __forceinline__ RowGrad grad_of(const PolicyRow &r, const PolicyArgs 
     return {sums.m, (-c + g * (H - log_s)) * per, kLn2 * g * per, c};
 }
 
-template <typename T>
-__global__ __launch_bounds__(kRowsPerBlock) void k_finish_policy(LogitsView x, RowsView rows, PolicyArgs args,
-                                                                 const RowPart *__restrict__ parts, int slices,
-                                                                 RowGrad *__restrict__ grad, double *__restrict__ sums)
-{
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + threadIdx.x;
-    const int tid = threadIdx.x;
-    __shared__ double wave[4][4];
-    PolicyRow r;
-    if (n < x.n) {
-        float l = 0.0f, H = 0.0f;
-        RowGrad g{0.0f, 0.0f, 0.0f, 0.0f};
-        const Place p = place_of(rows, n);
-        if (p.counts) {
-            const Sums a = merged_parts(parts + n * slices, slices);
-            const int act = args.actions[n];
-            const bool ok = act >= 0 && act < x.V;
-            float log_s;
-            finish_row(a, ok ? logit<T>(x, n, act) : 0.0f, ok, l, H, log_s);
-            if (ok && l != -INFINITY && a.s != 0.0f) {
-                RowIn in;
-                in.p = p;
-                policy_in(in, args, n);
-                r = policy_row(args, in, l, H);
-                g = grad_of(r, args, a, H, log_s);
-            }
-        }
-        if (grad) grad[n] = g;
-        if (args.out_logp) args.out_logp[n] = l;
-        if (args.out_entropy) args.out_entropy[n] = H;
-        if (args.out_coeff) args.out_coeff[n] = r.c * args.grad_scale;
-        if (args.out_entropy_coeff) args.out_entropy_coeff[n] = r.g * args.grad_scale;
-    }
-    const double v[4] = {wave_sum(r.sur), wave_sum(r.kl), wave_sum(r.H), wave_sum(r.cut)};
-    if ((tid & 63) == 0)
-        for (int i = 0; i < 4; ++i) wave[tid >> 6][i] = v[i];
-    __syncthreads();
-    if (tid < 4) sums[static_cast<size_t>(blockIdx.x) * 4 + tid] = wave[0][tid] + wave[1][tid] + wave[2][tid] + wave[3][tid];
-}
-
-__device__ __forceinline__ void policy_stats_out(const double (&v)[4], float kl_coeff, float entropy_coeff, float *out)
-{
-    out[0] = static_cast<float>(v[0] + kl_coeff * v[1] - entropy_coeff * v[2]);
-    for (int i = 0; i < 4; ++i) out[1 + i] = static_cast<float>(v[i]);
-}
-
 // 2^x (A + B x) of a slot
 template <int N>
 __device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g, const Ref &ref)
@@ -329,6 +246,12 @@ __device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g, const
             f[j] = exp2_of(x) * (g.A + g.B * fmaxf(x, kLowest));
         }
     }
+}
+
+__device__ __forceinline__ void policy_stats_out(const double (&v)[4], float kl_coeff, float entropy_coeff, float *out)
+{
+    out[0] = static_cast<float>(v[0] + kl_coeff * v[1] - entropy_coeff * v[2]);
+    for (int i = 0; i < 4; ++i) out[1 + i] = static_cast<float>(v[i]);
 }
 
 // ---- the loss from the workgroups' sums, in their order
@@ -588,6 +511,48 @@ __global__ __launch_bounds__(1024) void k_seq_totals(RowsView r, int seq_parts, 
             const int c = seq_n[q];
             weights[q] = c > 0 ? static_cast<float>(1.0 / (static_cast<double>(seqs) * c)) : 0.0f;
         }
+}
+
+// The weights of few rows under a mask in one launch by one workgroup (instead of two), a row to a thread.
+__global__ __launch_bounds__(1024) void k_weights(RowsView r, float *__restrict__ weight, float *__restrict__ weights)
+{
+    __shared__ int32_t bounds[kMiddleSeqs + 1];
+    __shared__ uint32_t count[kMiddleSeqs];
+    __shared__ int32_t wave[16];
+    const int tid = threadIdx.x;
+    if (r.bounds)
+        for (int q = tid; q < r.S + (r.order == PL_ROWS_PACKED); q += 1024) bounds[q] = r.bounds[q];
+    for (int q = tid; q < r.S; q += 1024) count[q] = 0;
+    __syncthreads();
+    if (r.bounds) r.bounds = bounds;
+    int n = 0;
+#pragma unroll 4
+    for (int64_t i = tid; i < r.n; i += 1024) {
+        const Place p = place_of(r, i);
+        n += p.counts;
+        if (weights && p.counts) atomicAdd(&count[p.seq], 1u);       // (whole numbers: their order does not matter)
+    }
+    auto total = [&](int v) {
+#pragma unroll
+        for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+        __syncthreads();
+        if ((tid & 63) == 0) wave[tid >> 6] = v;
+        __syncthreads();
+        v = 0;
+        for (int i = 0; i < 16; ++i) v += wave[i];
+        return v;
+    };
+    if (!weights) {
+        n = total(n);
+        if (tid == 0) *weight = n > 0 ? 1.0f / static_cast<float>(n) : 0.0f;
+        return;
+    }
+    __syncthreads();
+    int seqs = 0;
+    for (int q = tid; q < r.S; q += 1024) seqs += count[q] > 0;
+    seqs = total(seqs);
+    for (int q = tid; q < r.S; q += 1024)
+        weights[q] = count[q] > 0 ? static_cast<float>(1.0 / (static_cast<double>(seqs) * count[q])) : 0.0f;
 }
 
 // ---- pairs: margins, the loss, and d loss / d s of every sequence
@@ -1132,8 +1097,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
 // A lane holds CH slots of 16 aligned bytes, LANES apart, and one of the up to 2 N - 2 elements in front of the first and
 // behind the last whole slot.  Loads are predicated, with one value or -infinity in place of the others, so that all of
 // them are on their way before the first is waited for.
+// In launches of one width or another that were tried for rows of 32768 to 65536 bf16, workgroups of 256 and 512 threads with
+// sixteen slots to a lane came out first: several of them are on a compute unit, one loading while another computes
+// (8192 rows of 32768: 217 to 232 us; with 1024 threads and eight slots 272).
 template <typename T, int LANES, int CH, int PASS>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_waves_per_eu(CH == 16 ? 4 : 6))) void k_rows(RowArgs g)
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_waves_per_eu(4))) void k_rows(RowArgs g)
 {
     constexpr int N = Elem<T>::N, ROWS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / 64;
     constexpr bool kGrad = PASS == PASS_POLICY;
@@ -1345,6 +1313,35 @@ __global__ __launch_bounds__(256) void k_stream(RowArgs g, RowPart *__restrict__
     }
 }
 
+// What follows from the slices of rows, a row to a thread.
+template <typename T, int PASS>
+__global__ __launch_bounds__(kRowsPerBlock) void k_finish(RowArgs g, const RowPart *__restrict__ parts, int slices)
+{
+    __shared__ double sums[PASS == PASS_POLICY ? 4 : 1][256];
+    const int tid = threadIdx.x;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + tid;
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    if (n < g.x.n) {
+        RowIn in;
+        in.p = place_of(g.rows, n);
+        Sums a;
+        float z_a = 0.0f;
+        if (in.p.counts) {
+            in.act = g.actions[n];
+            read_in<PASS>(g, n, in);
+            if (in.act >= 0 && in.act < g.x.V) z_a = Elem<T>::load(static_cast<const T *>(g.x.data) + n * g.x.stride + in.act);
+            a = merged_parts(parts + n * slices, slices);
+        }
+        const RowGrad rg = finish_pass<PASS>(g, n, in, a, z_a, true, acc);
+        if (PASS == PASS_POLICY && g.grad) g.grad[n] = rg;
+    }
+    if constexpr (PASS == PASS_POLICY) {
+        for (int i = 0; i < 4; ++i) sums[i][tid] = acc[i];
+        __syncthreads();
+        finish_block_sums(g, sums);
+    }
+}
+
 // Slots of 16 bytes in a row, the last one begun; those of the rows that k_narrow and k_group take, and the rows of a workgroup of k_group.
 constexpr int kGroupSlots = 256;
 int row_slots(const LogitsView &x) { return x.dtype == PL_F32 ? (x.V + 3) / 4 : (x.V + 7) / 8; }
@@ -1354,13 +1351,17 @@ bool few_rows(const LogitsView &x) { return x.n < 64 && x.V >= 16384; }
 
 int row_blocks(int64_t n) { return static_cast<int>((n + kRowsPerBlock - 1) / kRowsPerBlock); }
 
-// Sums of the slices of every row into ws.parts.
-void launch_parts(const RowArgs &g, const LossWorkspace &ws, bool with_t, hipStream_t s)
+// Rows in slices: their sums into ws.parts, and what follows from them.
+template <int PASS>
+int launch_slices(const RowArgs &g, const LossWorkspace &ws, bool with_t, hipStream_t s)
 {
     by_type(g.x.dtype, [&](auto t) {
-        hipLaunchKernelGGL((k_stream<decltype(t), PASS_LOGP>), dim3(static_cast<uint32_t>(std::min<int64_t>(g.x.n, 2048)), ws.slices),
-                           dim3(256), 0, s, g, ws.parts, ws.slices, with_t);
+        using T = decltype(t);
+        hipLaunchKernelGGL((k_stream<T, PASS_LOGP>), dim3(static_cast<uint32_t>(std::min<int64_t>(g.x.n, 2048)), ws.slices), dim3(256), 0, s,
+                           g, ws.parts, ws.slices, with_t);
+        hipLaunchKernelGGL((k_finish<T, PASS>), dim3(row_blocks(g.x.n)), dim3(kRowsPerBlock), 0, s, g, ws.parts, ws.slices);
     });
+    return row_blocks(g.x.n);
 }
 
 void launch_grad(GradArgs a, hipStream_t s)
@@ -1418,6 +1419,10 @@ void launch_seq_sums(const RowsView &rows, const double *logp, const float *ref,
 void launch_weights(const RowsView &rows, bool by_seqs, const LossWorkspace &ws, hipStream_t s)
 {
     const int lanes_s = seq_lanes(rows);
+    if (rows.mask && rows.S <= kMiddleSeqs && rows.n <= kMiddleRows) {
+        hipLaunchKernelGGL(k_weights, dim3(1), dim3(1024), 0, s, rows, by_seqs ? nullptr : ws.weight, by_seqs ? ws.weights : nullptr);
+        return;
+    }
     if (rows.mask)
         hipLaunchKernelGGL(k_seq_sums, dim3((rows.S + lanes_s - 1) / lanes_s, ws.seq_parts), dim3(256), 0, s, rows, nullptr, nullptr,
                            lanes_s, nullptr, ws.seq_part_n);
@@ -1480,17 +1485,20 @@ int launch_rows(const RowArgs &g, hipStream_t s)
         else if (slots <= 64) group([&](auto stream) { go(k_group<T, 16, 4, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
         else if (slots <= 128) group([&](auto stream) { go(k_group<T, 16, 8, 2, PASS, decltype(stream)::value>, group_rows(slots)); });
         else if (slots <= 256) group([&](auto stream) { go(k_group<T, 64, 4, 4, PASS, decltype(stream)::value>, group_rows(slots)); });
-        if constexpr (PASS == PASS_PREF_GRAD) return;
-        else if (slots <= kGroupSlots) return;
-        else if (whole_slots <= 64 * 16) go_over(k_rows<T, 64, 16, PASS>, 4, 256);
-        else if (few_rows(g.x)) return;
-        else if constexpr (PASS == PASS_POLICY) {
-            if (whole_slots <= 256 * 16) go_over(k_rows<T, 256, 16, PASS>, 1, 256);
-            else if (whole_slots <= 512 * 16) go_over(k_rows<T, 512, 16, PASS>, 1, 512);
-            else if (whole_slots <= 1024 * 16) go_over(k_rows<T, 1024, 16, PASS>, 1, 1024);
-        } else {
-            blocks = static_cast<int>(std::min<int64_t>(g.x.n, 1 << 22));
-            hipLaunchKernelGGL((k_stream<T, PASS>), dim3(blocks), dim3(256), 0, s, g, nullptr, 1, g.out_entropy != nullptr);
+        if constexpr (PASS != PASS_PREF_GRAD) {
+            if (slots <= kGroupSlots || few_rows(g.x)) return;
+            if constexpr (PASS == PASS_POLICY) {
+                if (whole_slots <= 64 * 16) go_over(k_rows<T, 64, 16, PASS>, 4, 256);
+                else if (whole_slots <= 256 * 16) go_over(k_rows<T, 256, 16, PASS>, 1, 256);
+                else if (whole_slots <= 512 * 16) go_over(k_rows<T, 512, 16, PASS>, 1, 512);
+                else if (whole_slots <= 1024 * 16) go_over(k_rows<T, 1024, 16, PASS>, 1, 1024);
+            } else if (whole_slots <= 64 * 12) {
+                // (rows that are only read: 22336 of 3001 bf16 32 us, streamed 47; 8384 of 8000: 31 us, streamed 26)
+                go_over(k_rows<T, 64, 12, PASS>, 4, 256);
+            } else {
+                blocks = static_cast<int>(std::min<int64_t>(g.x.n, 1 << 22));
+                hipLaunchKernelGGL((k_stream<T, PASS>), dim3(blocks), dim3(256), 0, s, g, nullptr, 1, g.out_entropy != nullptr);
+            }
         }
     });
     return blocks;
@@ -1541,12 +1549,7 @@ void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_
     RowArgs g = row_args(x, rows, actions);
     g.out_logp = out_logp;
     g.out_entropy = out_entropy;
-    if (launch_rows<PASS_LOGP>(g, s)) return;
-    launch_parts(g, ws, out_entropy != nullptr, s);
-    by_type(x.dtype, [&](auto t) {
-        hipLaunchKernelGGL(k_finish_logp<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, actions, ws.parts,
-                           ws.slices, out_logp, out_entropy, nullptr, nullptr);
-    });
+    if (!launch_rows<PASS_LOGP>(g, s)) launch_slices<PASS_LOGP>(g, ws, out_entropy != nullptr, s);
 }
 
 void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &args, int reduction, float *out_stats,
@@ -1561,7 +1564,7 @@ void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyA
             (reduction == PL_REDUCE_SEQS ? a.weights : a.weight_at) = reduction == PL_REDUCE_SEQS ? ws.weights : ws.weight;
         }
     }
-    int blocks = row_blocks(x.n);
+    int blocks = 0;
     if (x.n > 0) {
         RowArgs g = row_args(x, rows, a.actions);
         g.policy = a;
@@ -1571,17 +1574,13 @@ void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyA
         g.out_stats = out_stats;
         g.out_grad = out_grad;
         g.grad_stride = grad_stride;
-        if (const int whole = launch_rows<PASS_POLICY>(g, s)) {
-            blocks = whole;
-            if (blocks == 1) return;             // the kernel has written the loss
-        } else {
-            launch_parts(g, ws, true, s);
-            by_type(x.dtype, [&](auto t) {
-                hipLaunchKernelGGL(k_finish_policy<decltype(t)>, dim3(blocks), dim3(kRowsPerBlock), 0, s, x, rows, a, ws.parts,
-                                   ws.slices, out_grad ? ws.grad : nullptr, ws.sums);
-            });
+        blocks = launch_rows<PASS_POLICY>(g, s);
+        if (!blocks) {
+            g.grad = out_grad ? ws.grad : nullptr;
+            blocks = launch_slices<PASS_POLICY>(g, ws, true, s);
             if (out_grad) launch_grad(grad_args(x, a.actions, ws, out_grad, grad_stride), s);
         }
+        if (blocks == 1) return;                 // the kernel has written the loss
     }
     hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, ws.sums, blocks, a.ref_logp ? a.kl_coeff : 0.0f,
                        a.entropy_coeff, out_stats);
@@ -1597,13 +1596,7 @@ void launch_preference_loss(const LogitsView &x, const RowsView &rows, const Pre
     // rows that are read fast again whole need nothing kept of them
     const bool again = row_slots(x) <= kGroupSlots;
     if (again) g.grad = nullptr;
-    if (x.n > 0 && !launch_rows<PASS_PREF_FORWARD>(g, s)) {
-        launch_parts(g, ws, false, s);
-        by_type(x.dtype, [&](auto t) {
-            hipLaunchKernelGGL(k_finish_logp<decltype(t)>, dim3(row_blocks(x.n)), dim3(kRowsPerBlock), 0, s, x, rows, a.actions,
-                               ws.parts, ws.slices, a.out_logp, nullptr, ws.logp, ws.grad);
-        });
-    }
+    if (x.n > 0 && !launch_rows<PASS_PREF_FORWARD>(g, s)) launch_slices<PASS_PREF_FORWARD>(g, ws, false, s);
     if (middle_fits(rows)) {
         hipLaunchKernelGGL(k_pref_middle, dim3(1), dim3(1024), 0, s, rows, a, ws.logp, seq_lanes(rows), ws.seq_coeff, out_stats);
     } else {
