@@ -101,27 +101,12 @@ __device__ __forceinline__ Sums rebased(const Sums &a, float m, const Ref &to)
     return {m, a.s * e, e * (a.t + fmaxf(d, kLowest) * a.s)};
 }
 
-__device__ __forceinline__ Sums merge(const Sums &a, const Sums &b)
-{
-    const float m = fmaxf(a.m, b.m);
-    const Ref to = ref_of(m);
-    const Sums x = rebased(a, m, to), y = rebased(b, m, to);
-    return {m, x.s + y.s, x.t + y.t};
-}
-
 template <int LANES>
 __device__ __forceinline__ Sums merge_of(const Sums &a)
 {
     const float m = max_of<LANES>(a.m);
     const Sums x = rebased(a, m, ref_of(m));
     return {m, sum_of<LANES>(x.s), sum_of<LANES>(x.t)};
-}
-
-__device__ __forceinline__ Sums merged_parts(const RowPart *parts, int slices)
-{
-    Sums a{parts[0].m, parts[0].s, parts[0].t};
-    for (int i = 1; i < slices; ++i) a = merge(a, Sums{parts[i].m, parts[i].s, parts[i].t});
-    return a;
 }
 
 // ---- rows and sequences
@@ -1313,13 +1298,13 @@ __global__ __launch_bounds__(256) void k_stream(RowArgs g, RowPart *__restrict__
     }
 }
 
-// What follows from the slices of rows, a row to a thread.
-template <typename T, int PASS>
-__global__ __launch_bounds__(kRowsPerBlock) void k_finish(RowArgs g, const RowPart *__restrict__ parts, int slices)
+// What follows from the slices of rows: a thread to a row of one slice, a wave to a row of several.
+template <typename T, int PASS, int LANES>
+__global__ __launch_bounds__(256) void k_finish(RowArgs g, const RowPart *__restrict__ parts, int slices)
 {
     __shared__ double sums[PASS == PASS_POLICY ? 4 : 1][256];
-    const int tid = threadIdx.x;
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + tid;
+    const int tid = threadIdx.x, lane = tid & (LANES - 1);
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + tid / LANES;
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
     if (n < g.x.n) {
         RowIn in;
@@ -1329,11 +1314,15 @@ __global__ __launch_bounds__(kRowsPerBlock) void k_finish(RowArgs g, const RowPa
         if (in.p.counts) {
             in.act = g.actions[n];
             read_in<PASS>(g, n, in);
+            if (lane < slices) {
+                const RowPart of = parts[n * slices + lane];
+                a = {of.m, of.s, of.t};
+            }
             if (in.act >= 0 && in.act < g.x.V) z_a = Elem<T>::load(static_cast<const T *>(g.x.data) + n * g.x.stride + in.act);
-            a = merged_parts(parts + n * slices, slices);
+            if constexpr (LANES > 1) a = merge_of<LANES>(a);
         }
-        const RowGrad rg = finish_pass<PASS>(g, n, in, a, z_a, true, acc);
-        if (PASS == PASS_POLICY && g.grad) g.grad[n] = rg;
+        const RowGrad rg = finish_pass<PASS>(g, n, in, a, z_a, lane == 0, acc);
+        if (PASS == PASS_POLICY && g.grad && lane == 0) g.grad[n] = rg;
     }
     if constexpr (PASS == PASS_POLICY) {
         for (int i = 0; i < 4; ++i) sums[i][tid] = acc[i];
@@ -1355,13 +1344,15 @@ int row_blocks(int64_t n) { return static_cast<int>((n + kRowsPerBlock - 1) / kR
 template <int PASS>
 int launch_slices(const RowArgs &g, const LossWorkspace &ws, bool with_t, hipStream_t s)
 {
+    const int blocks = static_cast<int>(ws.slices > 1 ? (g.x.n + 3) / 4 : row_blocks(g.x.n));
     by_type(g.x.dtype, [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL((k_stream<T, PASS_LOGP>), dim3(static_cast<uint32_t>(std::min<int64_t>(g.x.n, 2048)), ws.slices), dim3(256), 0, s,
                            g, ws.parts, ws.slices, with_t);
-        hipLaunchKernelGGL((k_finish<T, PASS>), dim3(row_blocks(g.x.n)), dim3(kRowsPerBlock), 0, s, g, ws.parts, ws.slices);
+        if (ws.slices > 1) hipLaunchKernelGGL((k_finish<T, PASS, 64>), dim3(blocks), dim3(256), 0, s, g, ws.parts, ws.slices);
+        else hipLaunchKernelGGL((k_finish<T, PASS, 1>), dim3(blocks), dim3(256), 0, s, g, ws.parts, 1);
     });
-    return row_blocks(g.x.n);
+    return blocks;
 }
 
 void launch_grad(GradArgs a, hipStream_t s)
