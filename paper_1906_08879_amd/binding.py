@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from typing import Optional
 
 import numpy as np
@@ -660,22 +661,23 @@ def clip_gradients(grads, max_norm: float, out_norm, out=None, workspace=None, s
     lib = load_library()
     grads = list(grads)
     n = len(grads)
-    numel = [g.numel() for g in grads]
-    dtypes = [g.dtype for g in grads]
+    numel, dtypes = [g.numel() for g in grads], [g.dtype for g in grads]
     if not all([g.is_cuda and g.is_contiguous() for g in grads]):
         raise PlacetoError("grads must be contiguous device tensors")
     codes = {t: _dtype_code(t, "grads") for t in set(dtypes)}
-    dst = None
+    # (arrays of the standard library are filled several times as fast as those of ctypes)
+    sources, results = array("Q", [g.data_ptr() for g in grads]), None
+    sizes, types = array("q", numel), array("i", [codes[t] for t in dtypes])
     if out is not None:
         out = list(out)
         if len(out) != n:
             raise PlacetoError(f"out has {len(out)} tensors, grads {n}")
         if not all([o.is_cuda and o.is_contiguous() for o in out]) or [o.dtype for o in out] != dtypes or [o.numel() for o in out] != numel:
             raise PlacetoError("out must be contiguous device tensors like their gradients")
-        dst = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out])
+        results = array("Q", [o.data_ptr() for o in out])
     ws, ws_bytes = _workspace(workspace, lib.pl_clip_gradients_workspace(n), out_norm.device, stream)
     _check(lib.pl_clip_gradients(
-        n, (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]), dst, (ctypes.c_int64 * n)(*numel),
-        (ctypes.c_int32 * n)(*[codes[t] for t in dtypes]), float(max_norm), _dev_ptr(out_norm, torch.float32, 1, "out_norm"),
-        ws.data_ptr(), ws_bytes, _stream_ptr(stream)), "pl_clip_gradients")
+        n, sources.buffer_info()[0], None if results is None else results.buffer_info()[0], sizes.buffer_info()[0],
+        types.buffer_info()[0], float(max_norm), _dev_ptr(out_norm, torch.float32, 1, "out_norm"), ws.data_ptr(), ws_bytes,
+        _stream_ptr(stream)), "pl_clip_gradients")
     return out_norm

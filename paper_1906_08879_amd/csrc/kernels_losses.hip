@@ -505,17 +505,29 @@ __global__ __launch_bounds__(1024) void k_weights(RowsView r, float *__restrict_
     __shared__ uint32_t count[kMiddleSeqs];
     __shared__ int32_t wave[16];
     const int tid = threadIdx.x;
+    uint8_t mask[8];                                     // of eight rows, 1024 apart
+    auto read_mask = [&](int64_t i) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mask[k] = r.mask[min(i + k * 1024, r.n - 1)];
+    };
+    read_mask(tid);
     if (r.bounds)
         for (int q = tid; q < r.S + (r.order == PL_ROWS_PACKED); q += 1024) bounds[q] = r.bounds[q];
     for (int q = tid; q < r.S; q += 1024) count[q] = 0;
     __syncthreads();
-    if (r.bounds) r.bounds = bounds;
+    RowsView in_lds = r;
+    if (r.bounds) in_lds.bounds = bounds;
+    in_lds.mask = nullptr;
     int n = 0;
-#pragma unroll 4
-    for (int64_t i = tid; i < r.n; i += 1024) {
-        const Place p = place_of(r, i);
-        n += p.counts;
-        if (weights && p.counts) atomicAdd(&count[p.seq], 1u);       // (whole numbers: their order does not matter)
+    for (int64_t i = tid; i < r.n; i += 8 * 1024) {
+        if (i != tid) read_mask(i);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k * 1024 < r.n && mask[k]) {
+                const Place p = place_of(in_lds, i + k * 1024);
+                n += p.counts;
+                if (weights && p.counts) atomicAdd(&count[p.seq], 1u);       // (whole numbers: their order does not matter)
+            }
     }
     auto total = [&](int v) {
 #pragma unroll
