@@ -962,7 +962,7 @@ __device__ __forceinline__ void keep_packed(uint4 &v) { asm volatile("" : "+v"(v
 
 // ---- rows of middling width: LANES lanes to a row, R rows of a lane one behind another, all of them in its registers; what
 // follows from the sums of the workgroup's rows is done a row to a thread, as for narrow rows: with a wave to a row it
-// took most of the time (131072 rows of 256 floats: 122 us, against 74).
+// took most of the time (131072 rows of 256 floats: 122 us, against 74; 56 with slots from the row's start).
 // A row is cut into slots of 16 bytes from its start, aligned or not; the last one is the row's last 16 bytes, some of which
 // the slot before has too: they are left out of the sums, and their gradient is written twice, the same.
 // STREAM: the gradient goes past the caches, where every row of it begins at a multiple of 16 bytes (65536 rows of 512
