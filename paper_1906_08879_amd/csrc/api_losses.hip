@@ -30,12 +30,10 @@ int view_logits(const pl_logits *in, LogitsView *x)
 
 int view_rows(const pl_rows *in, const LogitsView &x, RowsView *r)
 {
+    static const pl_rows one_sequence{1, PL_ROWS_BY_SEQ, nullptr, nullptr};
     *r = RowsView{};
     r->n = x.n;
-    if (!in) {
-        r->L = static_cast<int>(x.n);
-        return PL_OK;
-    }
+    if (!in) in = &one_sequence;
     if (in->order < PL_ROWS_BY_SEQ || in->order > PL_ROWS_PACKED) return fail(PL_ERR_SHAPE, "unknown order of rows");
     if (in->n_seqs < 1 || in->n_seqs > (1 << 23)) return fail(PL_ERR_SHAPE, "n_seqs must be 1 .. 2^23");
     r->S = in->n_seqs;
@@ -109,7 +107,7 @@ int pl_action_logp(const pl_logits *logits, const int32_t *actions, float *out_l
     if (int rc = view_rows(nullptr, x, &rows)) return rc;
     if (int rc = check_call(x, rows, actions, nullptr, 0, workspace, workspace_bytes, &ws)) return rc;
     if (!out_logp) return fail(PL_ERR_NULL, "out_logp is required");
-    launch_action_logp(x, actions, out_logp, out_entropy, ws, static_cast<hipStream_t>(stream));
+    launch_action_logp(x, rows, actions, out_logp, out_entropy, ws, static_cast<hipStream_t>(stream));
     PL_HIP(hipGetLastError());
     return PL_OK;
 }

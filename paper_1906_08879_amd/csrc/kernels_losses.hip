@@ -1543,12 +1543,9 @@ LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsVi
     return w;
 }
 
-void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_logp, float *out_entropy,
+void launch_action_logp(const LogitsView &x, const RowsView &rows, const int32_t *actions, float *out_logp, float *out_entropy,
                         const LossWorkspace &ws, hipStream_t s)
 {
-    RowsView rows;
-    rows.n = x.n;
-    rows.L = static_cast<int>(x.n);
     RowArgs g = row_args(x, rows, actions);
     g.out_logp = out_logp;
     g.out_entropy = out_entropy;

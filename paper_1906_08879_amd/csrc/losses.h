@@ -29,7 +29,7 @@ struct RowsView {
     const uint8_t *mask = nullptr;
     int64_t n = 0;
     int S = 1, L = 0, order = PL_ROWS_BY_SEQ;
-    uint32_t magic = 0;                // n / (S or L) = high word of n * magic, shifted right (for n < 2^31; 0: divided by 1)
+    uint32_t magic = 0;                // n / (S or L) = high word of n * magic, shifted right (for n < 2^31; 0: that is 1 or none)
     int shift = 0;
     bool all = true;                   // every row counts, known on the host
 };
@@ -85,7 +85,7 @@ struct LossWorkspace {
 LossWorkspace carve_loss_workspace(void *base, const LogitsView &x, const RowsView &rows);
 
 // csrc/kernels_losses.hip
-void launch_action_logp(const LogitsView &x, const int32_t *actions, float *out_logp, float *out_entropy,
+void launch_action_logp(const LogitsView &x, const RowsView &rows, const int32_t *actions, float *out_logp, float *out_entropy,
                         const LossWorkspace &ws, hipStream_t s);
 void launch_policy_loss(const LogitsView &x, const RowsView &rows, const PolicyArgs &a, int reduction, float *out_stats,
                         void *out_grad, int64_t grad_stride, const LossWorkspace &ws, hipStream_t s);
