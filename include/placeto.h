@@ -378,12 +378,13 @@ int pl_simulate_reward_ex(pl_graph_batch *g, int32_t D, const float *node_feats,
  *
  * Numbers: probabilities are taken in fp32 from logits of any type, sums over rows in float64;
  * gradients are rounded once to the logits' type.  Summation orders are fixed: equal inputs
- * give equal bits.  A logit of -inf (or of its type's lowest value beside larger ones) is an action
- * of probability zero.  Rows that do not count (pl_rows) are not used: whatever their logits,
- * actions or other entries hold, their outputs are zero.  A row that counts whose action is
- * outside [0, n_actions) or has probability zero adds nothing to a loss or a gradient (its
- * gradient is zero, its weight stays with the rows' number) and gets the log probability NaN
- * respectively -inf (NaN too where every logit of the row is -inf).  NaN and +inf logits of a row that counts give NaN: in its outputs and in the loss.
+ * give equal bits.  A logit of -inf is an action of probability zero, and so is one of its type's
+ * lowest value more than 150 ln 2 (104) below the row's largest, where its probability is no fp32
+ * number.  Rows that do not count (pl_rows) are not used: whatever their logits, actions or other
+ * entries hold, their outputs are zero.  A row that counts whose action is outside [0, n_actions) or
+ * has probability zero adds nothing to a loss or a gradient (its gradient is zero, its weight stays
+ * with the rows' number) and gets the log probability NaN respectively -inf (NaN too where every logit
+ * of the row is -inf).  NaN and +inf logits of a row that counts give NaN: in its outputs and in the loss.
  *
  * All arrays are device memory, calls are asynchronous on `stream`, allocate nothing and can be
  * captured into a HIP graph.  `workspace` is device memory of at least the bytes that the matching

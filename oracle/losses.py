@@ -30,9 +30,10 @@ def rows_of(n, n_seqs=1, order="by_seq", bounds=None, mask=None):
     return seq, counts
 
 
-def softmax_rows(logits, actions, counts=None):
+def softmax_rows(logits, actions, counts=None, lowest=None):
     """log probabilities [n, V], those of the actions and the entropies; rows that do not count are zero.
-    A row adds something (`live`) if its action exists and has a probability."""
+    A row adds something (`live`) if its action exists and has a probability.  `lowest`: the lowest value of the logits'
+    type, which stands for -inf where its probability relative to the largest logit's is below 2^-150."""
     z = np.asarray(logits, np.float64)
     n, V = z.shape
     counts = np.ones(n, bool) if counts is None else counts
@@ -45,6 +46,8 @@ def softmax_rows(logits, actions, counts=None):
             l[i] = H[i] = np.nan
             continue
         d = z[i] - z[i].max()
+        if lowest is not None:
+            d[(z[i] == lowest) & (d < -150.0 * np.log(2.0))] = -np.inf
         every[i] = d - np.log(np.exp(d).sum())
         p = np.exp(every[i])
         H[i] = -np.sum(p[p > 0] * every[i][p > 0])
@@ -69,10 +72,10 @@ def logits_gradient(every, actions, H, live, d_l, d_H):
 
 
 def policy_loss(logits, actions, advantages, rows=None, old=None, ref=None, clip_low=0.2, clip_high=0.2, kl_coeff=0.0,
-                entropy_coeff=0.0, reduction="rows", per_seq=False, grad_scale=1.0, n_seqs=1):
+                entropy_coeff=0.0, reduction="rows", per_seq=False, grad_scale=1.0, n_seqs=1, lowest=None):
     n = len(actions)
     seq, counts = rows if rows is not None else (np.zeros(n, np.int64), np.ones(n, bool))
-    every, l, H, live = softmax_rows(logits, actions, counts)
+    every, l, H, live = softmax_rows(logits, actions, counts, lowest)
     length = np.bincount(seq[counts], minlength=n_seqs)
     w = np.zeros(n)
     for i in np.flatnonzero(counts):
@@ -97,10 +100,10 @@ def policy_loss(logits, actions, advantages, rows=None, old=None, ref=None, clip
 
 
 def preference_loss(logits, actions, rows, n_seqs, pairs=None, ref=None, beta=0.1, smoothing=0.0, average=False,
-                    grad_scale=1.0):
+                    grad_scale=1.0, lowest=None):
     n = len(actions)
     seq, counts = rows
-    every, l, H, live = softmax_rows(logits, actions, counts)
+    every, l, H, live = softmax_rows(logits, actions, counts, lowest)
     length = np.bincount(seq[counts], minlength=n_seqs)
     per = np.where(average & (length > 0), 1.0 / np.maximum(length, 1), 1.0)
     total, ratio = np.zeros(n_seqs), np.zeros(n_seqs)

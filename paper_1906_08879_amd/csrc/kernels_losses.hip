@@ -20,6 +20,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr double kAddsNothing = INFINITY;   // in place of the l of a row that adds nothing to its sequence
 constexpr float kLowest = -300.0f;     // 2^-300 is 0 in fp32: an x below it stands for -infinity, whose product with 0 is NaN
+constexpr float kNoChance = -150.0f;   // 2^-150 rounds to 0 in fp32: an action at the type's lowest value is masked below it
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -157,6 +158,8 @@ __device__ __forceinline__ float reciprocal(float s)
     const float r = __builtin_amdgcn_rcpf(s);
     return __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
 }
+
+__device__ __forceinline__ float lowest_of(int dtype) { return dtype == PL_F32 ? -0x1.fffffep127f : dtype == PL_BF16 ? -0x1.fep127f : -65504.0f; }
 
 // l, H and log s of a row from its sums; a row without an allowed action has l = NaN, an action of probability zero
 // l = -infinity.
@@ -752,6 +755,7 @@ __device__ __forceinline__ RowGrad finish_pass(const RowArgs &g, int64_t n, cons
     bool live = false;
     if (in.p.counts) {
         const bool ok = in.act >= 0 && in.act < g.x.V;
+        if (z_a == lowest_of(g.x.dtype) && ref_of(a.m)(z_a) < kNoChance) z_a = -INFINITY;
         finish_row(a, z_a, ok, l, H, log_s);
         live = ok && l != -INFINITY && a.s != 0.0f;
     }

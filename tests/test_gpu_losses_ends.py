@@ -1,0 +1,84 @@
+"""The losses on rows of logits and gradient clipping where a term leaves fp32, an action has no probability or a sum is
+long, against their float64 oracle."""
+import numpy as np
+import pytest
+
+from oracle import losses as ol
+from tests.test_gpu_losses import U, _dev, _host, _logits, _state, _t, check_grad, check_rows, eps
+
+pytestmark = pytest.mark.gpu
+
+
+# --------------------------------------------------------------------------- masked by the lowest value
+def _lowest(dtype):
+    import torch
+    return float(torch.finfo(_t(dtype)).min)
+
+
+def _rows_with_masked_actions(rng, n, V, dtype):
+    """The first half of the rows take an action whose logit is the type's lowest value or -inf; and the next one takes
+    the lowest where nothing is larger."""
+    z, a = _state(rng, n, V, dtype)
+    a[:] = V // 2
+    low = _lowest(dtype)
+    z[0, V // 2] = low
+    z[1, V // 2] = -np.inf
+    z[2, V // 4:] = low                                   # as a padded vocabulary, the action among it
+    z[3] = low; z[3, 0] = -low
+    z[4] = low                                            # nothing larger: all equally likely
+    z[5] = -np.inf; z[5, V // 2] = low                    # the only action there is
+    return z, a, low
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", [4, 5, 37, 700, 9000, 70001, 140001])
+def test_an_action_masked_by_the_lowest_value_has_no_probability(V, dtype):
+    import torch
+    import paper_1906_08879_amd as pl
+    rng = np.random.default_rng(V)
+    n = 12
+    z, a, low = _rows_with_masked_actions(rng, n, V, dtype)
+    x, act = _logits(z, dtype), _dev(a)
+    _, l, H, live = ol.softmax_rows(z, a, lowest=low)
+    assert (l[:4] == -np.inf).all() and live[4:].all() and not live[:4].any()
+    logp, ent = torch.empty(n, device="cuda:0"), torch.empty(n, device="cuda:0")
+    pl.action_logp(x, act, logp, ent)
+    check_rows(_host(logp), l, V, "logp")
+    check_rows(_host(ent), H, V, "entropy")
+    finite = np.where(np.isfinite(l), l, 0.0)
+    old, ref = (finite + rng.normal(0, 0.1, n)).astype(np.float32), (finite + rng.normal(0, 0.3, n)).astype(np.float32)
+    adv = rng.normal(0, 1, n).astype(np.float32)
+    for o in (None, old):
+        stats, grad = torch.empty(5, device="cuda:0"), torch.full_like(x, 7.0)
+        kw = dict(kl_coeff=0.3, entropy_coeff=0.1, clip_low=1.0, clip_high=9.0)
+        pl.clipped_policy_loss(x, act, _dev(adv), stats, old_logp=None if o is None else _dev(o), ref_logp=_dev(ref), out_grad=grad,
+                               out_logp=logp, **kw)
+        out = ol.policy_loss(z, a, adv, old=o, ref=ref, lowest=low, **kw)
+        assert np.isfinite(out["stats"]).all() and (out["grad"][:4] == 0).all()
+        check_rows(_host(logp), out["logp"], V, "logp of the loss")
+        # per row: the surrogate and the KL estimate with e^d up to e^1, the entropy with its own size
+        tol = (eps(V, finite) * (4.0 * np.abs(adv) + 2.0 + H)).sum() * 2.0 / n
+        assert (np.abs(_host(stats) - out["stats"]) <= tol).all(), (_host(stats), out["stats"])
+        check_grad(_host(grad), dict(out, actions=a), (4.0 * np.abs(adv) + 2.0 + H) / n, dtype, "grad")
+    stats, grad, coeff = torch.empty(2, device="cuda:0"), torch.full_like(x, 7.0), torch.empty(n, device="cuda:0")
+    pl.preference_loss(x, act, pl.DecisionRows(n, 4), stats, ref_logp=_dev(ref), beta=0.5, out_grad=grad, out_logp=logp, out_coeff=coeff)
+    out = ol.preference_loss(z, a, ol.rows_of(n, 4), 4, ref=ref, beta=0.5, lowest=low)
+    check_rows(_host(logp), out["logp"], V, "logp of the preference")
+    tol = 0.5 * (eps(V, finite) * np.maximum(1.0, np.abs(finite))).sum() + 16 * U
+    assert (np.abs(_host(stats) - out["stats"]) <= tol).all() and (np.abs(_host(coeff) - out["coeff"]) <= tol).all()
+    assert (_host(grad)[:4] == 0).all() and (_host(coeff)[:4] == 0).all()
+    check_grad(_host(grad), dict(out, actions=a), np.abs(out["coeff"]) + tol / eps(V, finite), dtype, "grad of the preference")
+
+
+def test_the_lowest_half_precision_value_close_to_the_others_has_a_probability():
+    import torch
+    import paper_1906_08879_amd as pl
+    low = _lowest("fp16")
+    z = np.full((3, 20), low)
+    z[0, 3] = low + 32.0                                  # the next number: 32 nats
+    z[1, 3] = low + 96.0
+    z[2, 3] = low + 128.0                                 # e^-128 is no fp32 number
+    a, logp = np.zeros(3, np.int32), torch.empty(3, device="cuda:0")
+    pl.action_logp(_logits(z, "fp16"), _dev(a), logp)
+    check_rows(_host(logp), ol.softmax_rows(z, a, lowest=low)[1], 20, "logp")
+    assert _host(logp)[1] == -96.0 and _host(logp)[2] == -np.inf
