@@ -432,13 +432,14 @@ int pl_action_logp(const pl_logits *logits, const int32_t *actions, float *out_l
  * r = exp(l - old), d = ref - l, H the entropy of the row's distribution:
  *     value = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coeff (e^d - d - 1) - entropy_coeff H
  * and the loss is the sum over the rows that count of w times the value.  e^d - d - 1 >= 0 is the
- * estimate of KL(pi || ref) from samples of pi whose derivative is kl_coeff (1 - e^d).
+ * estimate of KL(pi || ref) from samples of pi whose derivative is kl_coeff (1 - e^d).  r and e^d are fp32
+ * numbers, infinite from e^88.7 on.
  *   reduction    PL_REDUCE_ROWS: w = 1 / rows that count; PL_REDUCE_SEQS: w = 1 / (sequences with such rows x
  *                rows of the sequence that count); PL_REDUCE_SUM: w = 1.  Nothing counts: loss and gradient are 0
  *   grad_scale   factor of every derivative below (1 for the plain gradient of the loss)
  *   advantages   dev [n_rows] fp32, or [n_seqs] with advantage_per_seq
  *   old_logp     dev [n_rows] fp32: of the policy that took the actions; NULL: this one (r = 1)
- *   ref_logp     dev [n_rows] fp32: of the reference; NULL: no KL term
+ *   ref_logp     dev [n_rows] fp32: of the reference; NULL: no KL term.  With kl_coeff 0 its estimate is reported only
  *   out_stats    dev [5] fp32: loss; sums of w times the clipped surrogate (with its sign in the loss), the
  *                KL estimate, the entropy; the share w of rows whose ratio was clipped
  *   out_grad     dev [n_rows, n_actions] of the logits' type, rows grad_stride elements apart: d loss / d logits.

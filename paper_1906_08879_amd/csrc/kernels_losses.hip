@@ -204,7 +204,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs &a, const RowIn
     if (a.ref_logp) {
         const float d = in.ref - l, e = expm1f(d);
         r.kl = in.w * (e - d);
-        r.c += a.kl_coeff * e;
+        r.c += a.kl_coeff != 0.0f ? a.kl_coeff * e : 0.0f;   // (e may be infinite; the same below)
     }
     r.c *= in.w;
     r.g = in.w * a.entropy_coeff;
@@ -238,7 +238,7 @@ __device__ __forceinline__ void grad_slot(float (&f)[N], const RowGrad &g, const
 
 __device__ __forceinline__ void policy_stats_out(const double (&v)[4], float kl_coeff, float entropy_coeff, float *out)
 {
-    out[0] = static_cast<float>(v[0] + kl_coeff * v[1] - entropy_coeff * v[2]);
+    out[0] = static_cast<float>(v[0] + (kl_coeff != 0.0f ? kl_coeff * v[1] : 0.0) - entropy_coeff * v[2]);
     for (int i = 0; i < 4; ++i) out[1 + i] = static_cast<float>(v[i]);
 }
 

@@ -82,3 +82,32 @@ def test_the_lowest_half_precision_value_close_to_the_others_has_a_probability()
     pl.action_logp(_logits(z, "fp16"), _dev(a), logp)
     check_rows(_host(logp), ol.softmax_rows(z, a, lowest=low)[1], 20, "logp")
     assert _host(logp)[1] == -96.0 and _host(logp)[2] == -np.inf
+
+
+# --------------------------------------------------------------------------- terms that are multiplied by nothing
+def _far_rows(V, dtype, row, shift):
+    """Rows, and log probabilities of another policy that are `shift` off in one row."""
+    rng = np.random.default_rng(V)
+    z, a = _state(rng, 12, V, dtype, 1.0)
+    other = (ol.softmax_rows(z, a)[1] + rng.normal(0, 0.1, 12)).astype(np.float32)
+    other[row] += np.float32(shift)
+    return rng, z, a, other
+
+
+@pytest.mark.parametrize("V", [4, 5, 37, 700, 9000, 70001, 140001])
+def test_a_reference_that_is_only_watched_adds_nothing(V):
+    """kl_coeff 0: the loss and the gradient are those without a reference, however far it lies; its estimate is reported."""
+    import torch
+    import paper_1906_08879_amd as pl
+    for shift in (100.0, 1000.0, -np.inf, np.nan):
+        rng, z, a, ref = _far_rows(V, "bf16", 3, shift)
+        x, act, adv = _logits(z, "bf16"), _dev(a), _dev(rng.normal(0, 1, 12).astype(np.float32))
+        got = []
+        for r in (None, _dev(ref)):
+            stats, grad, coeff = torch.empty(5, device="cuda:0"), torch.full_like(x, 7.0), torch.empty(12, device="cuda:0")
+            pl.clipped_policy_loss(x, act, adv, stats, ref_logp=r, entropy_coeff=0.1, out_grad=grad, out_coeff=coeff)
+            got.append((_host(stats), _host(grad), _host(coeff)))
+        (s0, g0, c0), (s1, g1, c1) = got
+        assert np.isfinite(s1[[0, 1, 3, 4]]).all() and (s0[[0, 1, 3, 4]] == s1[[0, 1, 3, 4]]).all(), (shift, s0, s1)
+        assert (g0 == g1).all() and (c0 == c1).all(), shift
+        assert np.isnan(s1[2]) if np.isnan(shift) else s1[2] == np.inf       # (e^100 is no fp32 number)
