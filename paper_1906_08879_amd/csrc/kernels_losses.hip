@@ -196,7 +196,8 @@ __device__ __forceinline__ void policy_in(RowIn &in, const PolicyArgs &a, int64_
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs &a, const RowIn &in, float l, float H)
 {
     PolicyRow r;
-    const float ratio = a.old_logp ? expf(l - in.old) : (l == l ? 1.0f : l);
+    float ratio = a.old_logp ? expf(l - in.old) : (l == l ? 1.0f : l);
+    if (in.adv == 0.0f && ratio == INFINITY) ratio = 0.0f;       // no advantage, whatever the ratio: not 0 times infinity
     const bool cut = in.adv > 0.0f ? ratio > 1.0f + a.clip_high : (in.adv < 0.0f && ratio < 1.0f - a.clip_low);
     const float held = cut ? (in.adv > 0.0f ? 1.0f + a.clip_high : 1.0f - a.clip_low) : ratio;
     r.sur = in.w * (-in.adv * held);

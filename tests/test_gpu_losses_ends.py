@@ -111,3 +111,24 @@ def test_a_reference_that_is_only_watched_adds_nothing(V):
         assert np.isfinite(s1[[0, 1, 3, 4]]).all() and (s0[[0, 1, 3, 4]] == s1[[0, 1, 3, 4]]).all(), (shift, s0, s1)
         assert (g0 == g1).all() and (c0 == c1).all(), shift
         assert np.isnan(s1[2]) if np.isnan(shift) else s1[2] == np.inf       # (e^100 is no fp32 number)
+
+
+@pytest.mark.parametrize("V", [4, 5, 37, 700, 9000, 70001, 140001])
+def test_no_advantage_whatever_the_ratio(V):
+    import torch
+    import paper_1906_08879_amd as pl
+    for shift in (-100.0, -np.inf):
+        rng, z, a, old = _far_rows(V, "bf16", 3, shift)
+        adv = rng.normal(0, 1, 12).astype(np.float32)
+        adv[3] = 0.0
+        x = _logits(z, "bf16")
+        stats, grad, coeff = torch.empty(5, device="cuda:0"), torch.full_like(x, 7.0), torch.empty(12, device="cuda:0")
+        pl.clipped_policy_loss(x, _dev(a), _dev(adv), stats, old_logp=_dev(old), out_grad=grad, out_coeff=coeff)
+        # (the ratio of row 3 in 64 bits is a number, or not: its product with 0 is 0)
+        old[3] = ol.softmax_rows(z, a)[1][3]
+        out = ol.policy_loss(z, a, adv, old=old)
+        size = np.abs(adv) * 2.0                          # ratios are e^(a few tenths), and held
+        tol = (eps(V, out["logp"]) * size).sum() * 2.0 / 12 + 8 * U * np.abs(out["stats"])
+        assert (np.abs(_host(stats) - out["stats"]) <= tol).all(), (_host(stats), out["stats"])
+        assert _host(coeff)[3] == 0 and (_host(grad)[3] == 0).all()
+        check_grad(_host(grad), dict(out, actions=a), size / 12, "bf16", (V, shift))
