@@ -117,7 +117,7 @@ def preference_loss(logits, actions, rows, n_seqs, pairs=None, ref=None, beta=0.
         if not (0 <= a < n_seqs and 0 <= b < n_seqs):
             continue
         m = margins[k] = beta * (ratio[a] - ratio[b])
-        loss += (1.0 - smoothing) * np.logaddexp(0.0, -m) + smoothing * np.logaddexp(0.0, m)
+        loss += sum(w * np.logaddexp(0.0, x) for w, x in ((1.0 - smoothing, -m), (smoothing, m)) if w != 0.0)
         right += m > 0
         valid += 1
         g = 1.0 / (1.0 + np.exp(-m)) - 1.0 + smoothing

@@ -586,6 +586,12 @@ __device__ __forceinline__ float d_margin(float m, float eps)
 
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))) + (x != x ? x : 0.0f); }
 
+// (A margin may be infinite: a term without weight is left out, not 0 times infinity.)
+__device__ __forceinline__ float pair_loss(float m, float eps)
+{
+    return (eps != 1.0f ? (1.0f - eps) * softplus(-m) : 0.0f) + (eps != 0.0f ? eps * softplus(m) : 0.0f);
+}
+
 // d loss / d s of the THREADS / kTeam sequences from q0 on, kTeam lanes to each: with a list of pairs they go over all of
 // them, THREADS at a time through LDS, and add those of their sequence; without one a sequence is in one pair.  `first`:
 // the loss and the margins as well.
@@ -612,7 +618,7 @@ __device__ __forceinline__ void pairs_of(const PrefArgs &p, int S, int q0, bool 
                 if (pr.ok) {
                     m = margin(pr);
                     g = d_margin(m, p.smoothing);
-                    if (first) loss += (1.0f - p.smoothing) * softplus(-m) + p.smoothing * softplus(m);
+                    if (first) loss += pair_loss(m, p.smoothing);
                     right += m > 0.0f;
                     valid += 1.0;
                 }

@@ -132,3 +132,31 @@ def test_no_advantage_whatever_the_ratio(V):
         assert (np.abs(_host(stats) - out["stats"]) <= tol).all(), (_host(stats), out["stats"])
         assert _host(coeff)[3] == 0 and (_host(grad)[3] == 0).all()
         check_grad(_host(grad), dict(out, actions=a), size / 12, "bf16", (V, shift))
+
+
+@pytest.mark.parametrize("V", [4, 37, 9000])
+@pytest.mark.parametrize("smoothing,side", [(0.0, 0), (1.0, 1)])
+@pytest.mark.parametrize("S", [4, 3000])
+def test_a_pair_that_is_certain_costs_nothing(V, smoothing, side, S):
+    """A reference of -inf makes a margin infinite; the term of the other order has no weight."""
+    import torch
+    import paper_1906_08879_amd as pl
+    if V * S > 200000:
+        V = 40
+    rng = np.random.default_rng(V + S)
+    n = 2 * S
+    z, a = _state(rng, n, V, "fp32", 1.0)
+    ref = (ol.softmax_rows(z, a)[1] + rng.normal(0, 0.1, n)).astype(np.float32)
+    ref[2 * side] = -np.inf                               # of the first or of the second sequence
+    for pairs in (None, np.array([[0, 1], [2, 3], [3, 2]], np.int32)):
+        stats, margins, coeff = torch.empty(2, device="cuda:0"), torch.empty(S // 2 if pairs is None else 3, device="cuda:0"), torch.empty(n, device="cuda:0")
+        grad = torch.empty((n, V), device="cuda:0")
+        pl.preference_loss(_logits(z, "fp32"), _dev(a), pl.DecisionRows(n, S), stats, pairs=None if pairs is None else _dev(pairs),
+                           ref_logp=_dev(ref), label_smoothing=smoothing, out_margins=margins, out_coeff=coeff, out_grad=grad)
+        out = ol.preference_loss(z, a, ol.rows_of(n, S), S, pairs=pairs, ref=ref, smoothing=smoothing)
+        assert out["margins"][0] == (-np.inf if side else np.inf) and np.isfinite(out["stats"]).all()
+        assert _host(margins)[0] == out["margins"][0]
+        # margins are beta = 0.1 times sums of four rows; the loss has a slope of at most 1 in them
+        tol = 0.1 * 4.0 * (eps(V, out["logp"]) * np.maximum(1.0, np.abs(out["logp"]))).max() + 16 * U
+        assert (np.abs(_host(stats) - out["stats"]) <= tol).all(), (_host(stats), out["stats"])
+        assert (_host(coeff)[:4] == 0).all() and np.isfinite(_host(coeff)).all() and (_host(grad)[:4] == 0).all()
