@@ -488,7 +488,8 @@ int pl_preference_loss(const pl_logits *logits, const pl_rows *rows, const pl_pr
 /* ---- the 2-norm of all gradients of a model together, and clipping to it:
  *     norm = sqrt(sum over tensors and elements of g^2),   clipped = g * (max_norm / norm) if norm > max_norm, else g
  * The sum is taken in float64 (no gradient overflows it, and its order is fixed), the product in fp32, rounded
- * once.  A norm that is NaN or infinite is reported and leaves the gradients as they are.
+ * once.  A norm that is NaN, infinite or above the largest fp32 number is reported (as NaN or infinity) and leaves the
+ * gradients as they are.
  *   n_tensors    >= 0
  *   grads        host [n_tensors] of dev pointers, aligned to their elements (NULL where numel is 0)
  *   clipped      host [n_tensors] of dev pointers for the results, or NULL: in place.  An entry may equal the

@@ -137,7 +137,8 @@ __device__ __forceinline__ double block_sum(double v)
     return v;
 }
 
-// max_norm / norm = m 2^e: the quotient of a tiny limit and a huge norm is no fp32 number, its products are.
+// max_norm / norm = m 2^e: the quotient of a tiny limit and a huge norm is no fp32 number, its products are.  One for a norm that
+// is reported as infinite or NaN.
 struct Factor {
     float m;
     int e;
@@ -147,7 +148,7 @@ struct Factor {
 __device__ __forceinline__ Factor factor_of(double norm, float max_norm)
 {
     Factor f{1.0f, 0};
-    if (norm > max_norm && norm < INFINITY) f.m = static_cast<float>(frexp(max_norm / norm, &f.e));
+    if (norm > max_norm && static_cast<float>(norm) < INFINITY) f.m = static_cast<float>(frexp(max_norm / norm, &f.e));
     return f;
 }
 

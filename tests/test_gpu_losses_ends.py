@@ -160,3 +160,16 @@ def test_a_pair_that_is_certain_costs_nothing(V, smoothing, side, S):
         tol = 0.1 * 4.0 * (eps(V, out["logp"]) * np.maximum(1.0, np.abs(out["logp"]))).max() + 16 * U
         assert (np.abs(_host(stats) - out["stats"]) <= tol).all(), (_host(stats), out["stats"])
         assert (_host(coeff)[:4] == 0).all() and np.isfinite(_host(coeff)).all() and (_host(grad)[:4] == 0).all()
+
+
+# --------------------------------------------------------------------------- clipping
+def test_a_norm_above_fp32_is_reported_and_leaves_the_gradients():
+    import torch
+    import paper_1906_08879_amd as pl
+    for size in (4, 40000, 3000000):
+        g = torch.full((size,), 3e38, device="cuda:0")
+        before, out, norm = g.clone(), torch.full_like(g, 7.0), torch.empty(1, device="cuda:0")
+        pl.clip_gradients([g], 1.0, norm, out=[out])
+        assert float(norm) == float("inf") and torch.equal(out, before)
+        pl.clip_gradients([g], 1.0, norm)
+        assert float(norm) == float("inf") and torch.equal(g, before)
