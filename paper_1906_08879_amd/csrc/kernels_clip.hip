@@ -72,15 +72,10 @@ struct ListChunks {
 __device__ __forceinline__ TableChunks chunks_of(const ClipTable &t) { return TableChunks(t); }
 __device__ __forceinline__ ListChunks chunks_of(const ClipList &t) { return ListChunks(t); }
 
-// Squares of a slot: in fp32 where their sum is well within its range, which all but wild or vanished gradients are (one
-// conversion to a slot instead of one to an element, which took longer than the elements' bytes), else in float64.
+// Squares of a slot in float64.
 template <int N>
 __device__ __forceinline__ double slot_squares(const float (&f)[N])
 {
-    float s = 0.0f;
-#pragma unroll
-    for (int k = 0; k < N; ++k) s = __builtin_fmaf(f[k], f[k], s);
-    if (s > 0x1p-90f && s < 0x1p120f) return s;
     double d = 0.0;
 #pragma unroll
     for (int k = 0; k < N; ++k) d = __builtin_fma(static_cast<double>(f[k]), static_cast<double>(f[k]), d);
