@@ -139,7 +139,8 @@ __device__ __forceinline__ Place place_of(const RowsView &r, int64_t n)
     return p;
 }
 
-// l of a row to more than fp32: the sums over a sequence, whose difference to another one's counts, see no rounding of l.
+// l of a row from its fp32 maximum and sum, not rounded itself: sums over a sequence, whose difference to another one's counts, are
+// off by what s is off (some units of 2^-24), not by that of l's own size.
 __device__ __forceinline__ double exact_l(const Sums &a, float z_a)
 {
     return (static_cast<double>(z_a) - a.m) - log(static_cast<double>(a.s));
@@ -1228,7 +1229,9 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
 }
 
 // ---- long rows, or slices of them where there are few, that are only read: a workgroup to a row (slice), a few slots of a
-// lane on their way while the ones before are added.  A lane's x are relative to the largest logit that it has seen.
+// lane on their way while the ones before are added.  A lane's x are relative to the largest logit that it has seen.  Its sums are
+// fp32 over a step (16 or 32 logits) and float64 over the steps: in fp32 alone equal logits all round the same way (rows of 2^22 of
+// them: log probabilities off by 2e-4).
 constexpr int kStreamSlots = 4;
 
 template <typename T, bool WITH_T>
@@ -1236,16 +1239,28 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
 {
     constexpr int N = Elem<T>::N, STEP = kStreamSlots * 256;
     const int tid = threadIdx.x;
-    Sums a;
+    Sums a;                                              // of a step, and
+    double s = 0.0, t = 0.0;                             // of the steps before, both relative to a.m
     Ref ref = ref_of(a.m);
-    auto rebase = [&](float m) {
-        a = rebased(a, m, ref_of(m));
-        ref = ref_of(m);
+    auto rebase = [&](float m) {                         // (as `rebased`, between two steps)
+        const Ref to = ref_of(m);
+        if (s != 0.0) {
+            const float d = to(ref.m), e = exp2_of(d);
+            t = e * (t + fmaxf(d, kLowest) * s);
+            s *= e;
+        }
+        a.m = m;
+        ref = to;
     };
     auto add_one = [&](float z) {
         const float x = ref(z), e = exp2_of(x);
         a.s += e;
         if (WITH_T) a.t += e * fmaxf(x, kLowest);
+    };
+    auto end_step = [&]() {
+        s += a.s;
+        if (WITH_T) t += a.t;
+        a.s = a.t = 0.0f;
     };
     uint4 next[kStreamSlots];
     if (begin < end) {
@@ -1257,6 +1272,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
         const float z = e >= 0 ? Elem<T>::load(row.p + e) : -INFINITY;
         if (z > a.m) rebase(z);
         if (e >= 0) add_one(z);
+        end_step();
     }
     for (int i = begin + tid; i - tid < end; i += STEP) {
         uint4 v[kStreamSlots];
@@ -1279,8 +1295,9 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
 #pragma unroll
                 for (int j = 0; j < N; ++j) add_one(f[j]);
             }
+        end_step();
     }
-    return merge_of<64>(a);
+    return merge_of<64>(Sums{a.m, static_cast<float>(s), static_cast<float>(t)});
 }
 
 // PASS_LOGP and PASS_PREF_FORWARD of whole rows, or (slices > 1) the sums of the slices.

@@ -162,6 +162,29 @@ def test_a_pair_that_is_certain_costs_nothing(V, smoothing, side, S):
         assert (_host(coeff)[:4] == 0).all() and np.isfinite(_host(coeff)).all() and (_host(grad)[:4] == 0).all()
 
 
+# --------------------------------------------------------------------------- long rows
+@pytest.mark.parametrize("V", [1 << 18, 1 << 22])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_many_equal_logits_do_not_add_up_to_an_error(V, dtype):
+    """Rows whose probabilities are equal but for the first ones (so many that every thread has met the largest logit): their
+    roundings all go the same way.  From the formulas: s = first + (V - first) e^-c.  A term is off by the roundings of x and of its exponent (4 U), a sum by those of a few dozen additions one
+    behind another, of lanes, waves and the logarithm: the 64 U of EPS without a share that grows with V."""
+    import torch
+    import paper_1906_08879_amd as pl
+    n, first, c = 64, 2048, np.array([0.40625, 1.3125, 2.71875, 5.15625])        # (numbers of bf16)
+    c = np.tile(c, n // 4)
+    x = torch.empty((n, V), dtype=_t(dtype), device="cuda:0")
+    x.copy_(-_dev(c).to(_t(dtype))[:, None].expand(n, V))
+    x[:, :first] = 0.0
+    logp, ent = torch.empty(n, device="cuda:0"), torch.empty(n, device="cuda:0")
+    pl.action_logp(x, _dev(np.full(n, 17, np.int32)), logp, ent)
+    s = first + (V - first) * np.exp(-c)
+    l, H = -np.log(s), np.log(s) + (V - first) * np.exp(-c) / s * c
+    tol = U * (64.0 + 4.0 * np.abs(l))
+    assert (np.abs(_host(logp) - l) <= tol).all(), (np.abs(_host(logp) - l) / tol).max()
+    assert (np.abs(_host(ent) - H) <= 2.0 * tol + 64.0 * U * c).all(), (np.abs(_host(ent) - H) / tol).max()
+
+
 # --------------------------------------------------------------------------- clipping
 def test_a_norm_above_fp32_is_reported_and_leaves_the_gradients():
     import torch
