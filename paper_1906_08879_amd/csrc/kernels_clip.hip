@@ -245,8 +245,6 @@ __global__ __launch_bounds__(kClipTensors) void k_clip_list(ClipTable t, ClipLis
 
 }  // namespace
 
-int clip_blocks(int64_t chunks) { return static_cast<int>(std::min<int64_t>(chunks, kClipBlocks)); }
-
 void launch_clip_list(const ClipTable &t, const ClipList &list, int at, hipStream_t s)
 {
     hipLaunchKernelGGL(k_clip_list, dim3(1), dim3(kClipTensors), 0, s, t, list, at);
@@ -255,7 +253,7 @@ void launch_clip_list(const ClipTable &t, const ClipList &list, int at, hipStrea
 template <typename Tensors>
 void launch_clip(const Tensors &t, int64_t chunks, double *sums, float max_norm, bool scales, float *out_norm, hipStream_t s)
 {
-    const int blocks = clip_blocks(chunks);
+    const int blocks = static_cast<int>(std::min<int64_t>(chunks, kClipBlocks));
     if (blocks) hipLaunchKernelGGL(k_clip_sums<Tensors>, dim3(blocks), dim3(256), 0, s, t, sums);
     if (blocks && scales)
         hipLaunchKernelGGL(k_clip_scale<Tensors>, dim3(blocks), dim3(256), 0, s, t, sums, blocks, max_norm, out_norm);

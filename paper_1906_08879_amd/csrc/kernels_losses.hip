@@ -835,8 +835,7 @@ __device__ __forceinline__ void finish_block_sums(const RowArgs &g, double (*sum
 // ---- narrow rows (up to kNarrow actions): a row per thread, 256 rows through LDS, everything in one pass.
 // The rows' elements go in and out in the order they lie in memory, whatever their number; rows are an odd number
 // of words apart in LDS, so that the lanes' walks along their rows meet 32 different banks.
-// One pass over the elements of rows [n0, n0 + count): f(row, column, element in memory), in 16-byte slots where the rows lie
-// behind one another.
+// The elements of rows [n0, n0 + count) into the tile or out of it, in 16-byte slots where the rows lie behind one another.
 template <typename T, bool STORE>
 __device__ __forceinline__ void narrow_tile(const void *data, int64_t stride, int64_t n0, int count, int V, uint32_t magic, int pitch,
                                             float *tile)
@@ -1112,15 +1111,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
 template <typename T, int LANES, int CH, int PASS>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_waves_per_eu(4))) void k_rows(RowArgs g)
 {
+    static_assert(LANES == 64 || LANES >= 256, "a wave or a workgroup to a row");
     constexpr int N = Elem<T>::N, ROWS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / 64;
     constexpr bool kGrad = PASS == PASS_POLICY;
-    __shared__ RowPart part[WAVES > 1 ? WAVES : 1];
+    __shared__ RowPart part[WAVES];
     __shared__ RowGrad shared_grad;
     __shared__ double loss[ROWS][4];               // of the rows that these lanes have had
     const int tid = threadIdx.x;
     int lane = tid & (LANES - 1);
     const int V = g.x.V;
-    const int mine = LANES < 64 ? tid / LANES : LANES == 64 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
+    const int mine = WAVES == 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
     if (PASS == PASS_POLICY && lane < 4) loss[mine][lane] = 0.0;
     if (PASS == PASS_POLICY) __syncthreads();
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * ROWS + mine; n < g.x.n; n += static_cast<int64_t>(gridDim.x) * ROWS) {
@@ -1141,12 +1141,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
                 if (k * LANES < whole) v[k] = row.load(k * LANES + lane);
             if (edge >= 0) z_edge = Elem<T>::load(row.p + edge);
             if (acts) z_a = Elem<T>::load(row.p + act);
-            constexpr int G = LANES < 64 ? LANES : 64;
             uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
 #pragma unroll
             for (int k = 0; k < CH; ++k)
                 if (k * LANES < whole) add_words<T>(v[k], most, least);
-            a.m = max_of<G>(fmaxf(z_edge, Elem<T>::largest(most, least)));
+            a.m = max_of<64>(fmaxf(z_edge, Elem<T>::largest(most, least)));
             const Ref ref = ref_of(a.m);
             auto add_all = [&](auto with_t) {
                 auto add_one = [&](float z) {
@@ -1165,13 +1164,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
                     }
                     if (kGrad) keep_packed(v[k]);
                 }
-                a.s = sum_of<G>(a.s);
-                if (with_t) a.t = sum_of<G>(a.t);
+                a.s = sum_of<64>(a.s);
+                if (with_t) a.t = sum_of<64>(a.t);
             };
             if (PASS == PASS_POLICY || (PASS == PASS_LOGP && g.out_entropy)) add_all(std::true_type{});
             else add_all(std::false_type{});
         }
-        if (WAVES <= 1 || tid < 64) read_in<PASS>(g, n, in);
+        if (WAVES == 1 || tid < 64) read_in<PASS>(g, n, in);
         RowGrad rg;
         if (WAVES > 1) {
             if ((tid & 63) == 0) part[tid >> 6] = {a.m, a.s, a.t};

@@ -119,7 +119,6 @@ struct ClipList {
     int32_t n, chunk, chunks;
 };
 
-int clip_blocks(int64_t chunks);       // workgroups, and partial sums, of a launch
 // The tensors of a table, from number `at` of the list on; the last call's table ends the list.
 void launch_clip_list(const ClipTable &t, const ClipList &list, int at, hipStream_t s);
 template <typename Tensors>            // ClipTable or ClipList
