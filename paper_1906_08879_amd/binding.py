@@ -636,9 +636,9 @@ def preference_loss(logits, actions, rows: DecisionRows, out_stats, pairs=None, 
     ref, rows_ref = ctypes.byref(view), _rows_ref(rows, n)
     grad, grad_stride = _out_grad(out_grad, logits)
     n_seqs = rows.n_seqs if rows is not None else 1
+    if pairs is not None and (not isinstance(pairs, torch.Tensor) or pairs.dim() != 2 or pairs.shape[1] != 2):
+        raise PlacetoError(f"pairs: expected a device tensor [n_pairs, 2], got {tuple(getattr(pairs, 'shape', ()))}")
     n_pairs = n_seqs // 2 if pairs is None else int(pairs.shape[0])
-    if pairs is not None and (pairs.dim() != 2 or pairs.shape[1] != 2):
-        raise PlacetoError(f"pairs: expected [n_pairs, 2], got {tuple(pairs.shape)}")
     if pairs is None and n_seqs % 2:
         raise PlacetoError("without pairs the number of sequences must be even")
     cfg = PreferenceCfg(beta, label_smoothing, grad_scale, int(average))
@@ -653,6 +653,15 @@ def preference_loss(logits, actions, rows: DecisionRows, out_stats, pairs=None, 
     return out_stats
 
 
+def _device_tensors(tensors, refusal):
+    try:
+        fine = all([t.is_cuda and t.is_contiguous() for t in tensors])
+    except AttributeError:
+        fine = False
+    if not fine:
+        raise PlacetoError(refusal)
+
+
 def clip_gradients(grads, max_norm: float, out_norm, out=None, workspace=None, stream=None):
     """pl_clip_gradients on device tensors: the 2-norm of all gradients together into out_norm [1], and the
     gradients clipped to max_norm, in place or into the tensors of `out`.  Tensors are fp32, bf16 or fp16 and
@@ -661,9 +670,10 @@ def clip_gradients(grads, max_norm: float, out_norm, out=None, workspace=None, s
     lib = load_library()
     grads = list(grads)
     n = len(grads)
+    if not isinstance(out_norm, torch.Tensor):
+        raise PlacetoError("out_norm must be a device tensor")
+    _device_tensors(grads, "grads must be contiguous device tensors")
     numel, dtypes = [g.numel() for g in grads], [g.dtype for g in grads]
-    if not all([g.is_cuda and g.is_contiguous() for g in grads]):
-        raise PlacetoError("grads must be contiguous device tensors")
     codes = {t: _dtype_code(t, "grads") for t in set(dtypes)}
     # (arrays of the standard library are filled several times as fast as those of ctypes)
     sources, results = array("Q", [g.data_ptr() for g in grads]), None
@@ -672,7 +682,8 @@ def clip_gradients(grads, max_norm: float, out_norm, out=None, workspace=None, s
         out = list(out)
         if len(out) != n:
             raise PlacetoError(f"out has {len(out)} tensors, grads {n}")
-        if not all([o.is_cuda and o.is_contiguous() for o in out]) or [o.dtype for o in out] != dtypes or [o.numel() for o in out] != numel:
+        _device_tensors(out, "out must be contiguous device tensors like their gradients")
+        if [o.dtype for o in out] != dtypes or [o.numel() for o in out] != numel:
             raise PlacetoError("out must be contiguous device tensors like their gradients")
         results = array("Q", [o.data_ptr() for o in out])
     ws, ws_bytes = _workspace(workspace, lib.pl_clip_gradients_workspace(n), out_norm.device, stream)

@@ -47,3 +47,13 @@ def test_a_sequence_compared_with_itself(n, V):
     assert abs(float(stats[0]) - np.log(2.0)) <= 4 * U and float(stats[1]) == 0.0
     assert abs(float(seq) - l.sum()) <= (eps(V, l) * np.maximum(1.0, np.abs(l))).sum() + 2 * U * np.abs(l.sum())
     assert (_host(grad) == 0).all() and (_host(coeff) == 0).all()
+
+
+def test_pairs_that_are_no_list_of_pairs_are_refused():
+    import torch
+    import paper_1906_08879_amd as pl
+    x, a, stats = torch.zeros((4, 3), device="cuda:0"), _dev(np.zeros(4, np.int32)), torch.empty(2, device="cuda:0")
+    for pairs in (_dev(np.int32(1)), _dev(np.zeros(2, np.int32)), _dev(np.zeros((1, 3), np.int32)), _dev(np.zeros((1, 2), np.int64)),
+                  torch.zeros((1, 2), dtype=torch.int32), [[0, 1]]):
+        with pytest.raises(pl.PlacetoError):
+            pl.preference_loss(x, a, pl.DecisionRows(4, 2), stats, pairs=pairs)

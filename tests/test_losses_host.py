@@ -147,3 +147,10 @@ def test_binding_refuses_tensors_off_the_device():
     with pytest.raises(pl.PlacetoError):
         pl.DecisionRows(4, 2, bounds=torch.zeros(2, dtype=torch.int32))
     assert np.isfinite(pl.load_library().pl_clip_gradients_workspace(3))
+
+
+@pytest.mark.parametrize("grads,norm,out", [([], None, None), ([np.zeros(3, np.float32)], "norm", None), ([None], "norm", None), ([], "norm", [None])])
+def test_binding_refuses_what_is_no_tensor(grads, norm, out):
+    import torch
+    with pytest.raises(pl.PlacetoError):
+        pl.clip_gradients(grads, 1.0, torch.zeros(1) if norm else None, out=out)
