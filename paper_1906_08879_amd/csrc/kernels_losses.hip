@@ -687,12 +687,13 @@ __global__ __launch_bounds__(256) void k_pairs(PrefArgs p, int S, const double *
     pairs_of<256>(p, S, blockIdx.x * (256 / kTeam), blockIdx.x == 0, seq_sum, seq_n, seq_coeff, out_stats);
 }
 
-// Few rows: the sums of sequences and the pairs in one launch by one workgroup (instead of three).
+// Few rows and sequences: the sums of sequences and the pairs in one launch by one workgroup (instead of three).
 __global__ __launch_bounds__(1024) void k_pref_middle(RowsView rows, PrefArgs p, const double *__restrict__ logp, int lanes_s,
                                                       float *__restrict__ seq_coeff, float *__restrict__ out_stats)
 {
-    __shared__ double seq_sum[2 * kMiddleSeqs];
-    __shared__ int32_t seq_n[kMiddleSeqs];
+    static_assert(kPairSeqs <= 1024 / kTeam, "all sequences at once");
+    __shared__ double seq_sum[2 * kPairSeqs];
+    __shared__ int32_t seq_n[kPairSeqs];
     const int tid = threadIdx.x;
     if (rows.order == PL_ROWS_BY_STEP) {
         for (int q0 = 0; q0 < rows.S; q0 += lanes_s) {
@@ -721,7 +722,7 @@ __global__ __launch_bounds__(1024) void k_pref_middle(RowsView rows, PrefArgs p,
         }
     }
     __syncthreads();
-    for (int q0 = 0; q0 < rows.S; q0 += 1024 / kTeam) pairs_of<1024>(p, rows.S, q0, q0 == 0, seq_sum, seq_n, seq_coeff, out_stats);
+    pairs_of<1024>(p, rows.S, 0, true, seq_sum, seq_n, seq_coeff, out_stats);
 }
 
 // What a kernel that takes whole rows does with them.
@@ -1408,12 +1409,14 @@ void launch_grad(GradArgs a, hipStream_t s)
     });
 }
 
-// Whether one workgroup does the sums of sequences and the pairs.  By step, its threads share a sequence's rows (64 sequences
-// of 200 steps: 19 us a call against 25 with three launches); otherwise a wave has a sequence to itself, which is slower
-// than two launches more (24 sequences of 256 rows: 18 us against 10) unless they are very few.
+// Whether one workgroup does the sums of sequences and the pairs: where the sequences are few, whatever the pairs.  By step, its
+// threads share a sequence's rows; otherwise a wave has a sequence to itself.  Kernels of one call, four logits a row, one workgroup
+// against two launches or three: by step 64 sequences of 30 rows 12.1 us against 11.6, of 200 rows 14.0 against 15.7 (and 19 against
+// 25 as a call), with 4096 pairs 57 against 67, with 131072 1390 against 1662, but 512 sequences of 4 rows 26 against 12, with 4096 pairs
+// 168 against 54; packed, 16 sequences of 100 rows 13.2 against 13.6, 64 of 30 20.4 against 14.1.
 bool middle_fits(const RowsView &rows)
 {
-    return rows.S <= kMiddleSeqs && rows.n <= (rows.order == PL_ROWS_BY_STEP ? kMiddleRows : kMiddleRows / 16);
+    return rows.order == PL_ROWS_BY_STEP ? rows.S <= kPairSeqs && rows.n <= kMiddleRows : rows.S <= kPairSeqs / 4 && rows.n <= kMiddleRows / 16;
 }
 
 GradArgs grad_args(const LogitsView &x, const int32_t *actions, const LossWorkspace &ws, void *out, int64_t out_stride)
