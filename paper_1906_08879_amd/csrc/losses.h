@@ -12,9 +12,9 @@ constexpr int kMaxActions = 1 << 24;
 constexpr int kNarrow = 16;            // actions of rows that a thread takes
 constexpr int kMaxSlices = 64;         // parts that a row is cut into where there are few rows
 constexpr int kRowsPerBlock = 256;     // rows of a workgroup of the per-row kernels
-constexpr int kMiddleRows = 32768;     // rows whose weights, or sums and pairs, one workgroup does
-constexpr int kMiddleSeqs = 1024;      // and sequences: for the weights
-constexpr int kPairSeqs = 64;          // for sums and pairs
+constexpr int kMiddleRows = 32768;     // rows, and sequences, whose sums and pairs one workgroup does
+constexpr int kPairSeqs = 64;
+constexpr int kMiddleSeqs = 1024;      // sequences whose rows one workgroup counts
 constexpr int kMaxSumBlocks = 2048;    // workgroups of the kernels that go over several rows
 constexpr int kMaxSeqParts = 128;      // parts that the rows of a sequence are cut into
 
