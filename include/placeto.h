@@ -389,13 +389,14 @@ int pl_simulate_reward_ex(pl_graph_batch *g, int32_t D, const float *node_feats,
  * All arrays are device memory, calls are asynchronous on `stream`, allocate nothing and can be
  * captured into a HIP graph.  `workspace` is device memory of at least the bytes that the matching
  * _workspace function names, 16-byte aligned, for the duration of the call (a call
- * leaves nothing in it that a later one reads); calls that overlap in time need one each. */
+ * leaves nothing in it that a later one reads); calls that overlap in time need one each.  Outputs do not
+ * overlap one another, the inputs or the workspace, but for out_grad and the logits where that is said. */
 enum { PL_F32 = 0, PL_BF16 = 1, PL_F16 = 2 };
 
 typedef struct {
     const void *data;       /* dev, [n_rows, n_actions] of `dtype`, aligned to its elements        */
     int64_t n_rows;         /* 0 .. 2^31 - 1                                                       */
-    int64_t row_stride;     /* elements from a row to the next, >= n_actions                       */
+    int64_t row_stride;     /* elements from a row to the next, n_actions .. 2^31                  */
     int32_t n_actions;      /* 1 .. 2^24                                                           */
     int32_t dtype;          /* PL_F32, PL_BF16 or PL_F16                                           */
 } pl_logits;
@@ -442,7 +443,8 @@ int pl_action_logp(const pl_logits *logits, const int32_t *actions, float *out_l
  *   ref_logp     dev [n_rows] fp32: of the reference; NULL: no KL term.  With kl_coeff 0 its estimate is reported only
  *   out_stats    dev [5] fp32: loss; sums of w times the clipped surrogate (with its sign in the loss), the
  *                KL estimate, the entropy; the share w of rows whose ratio was clipped
- *   out_grad     dev [n_rows, n_actions] of the logits' type, rows grad_stride elements apart: d loss / d logits.
+ *   out_grad     dev [n_rows, n_actions] of the logits' type, rows grad_stride elements (n_actions .. 2^31) apart:
+ *                d loss / d logits.
  *                May be the logits themselves (same stride); NULL to skip
  *   out_logp, out_entropy  dev [n_rows] fp32 or NULL
  *   out_coeff, out_entropy_coeff  dev [n_rows] fp32 or NULL: minus d loss / d l and minus d loss / d H,
