@@ -1229,10 +1229,12 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) __attribute__((amdgpu_wa
 }
 
 // ---- long rows, or slices of them where there are few, that are only read: a workgroup to a row (slice), a few slots of a
-// lane on their way while the ones before are added.  A lane's x are relative to the largest logit that it has seen.  Its sums are
-// fp32 over a step (16 or 32 logits) and float64 over the steps: in fp32 alone equal logits all round the same way (rows of 2^22 of
-// them: log probabilities off by 2e-4).
+// lane on their way while the ones before are added.  A lane's sums are fp32 over a step (16 or 32 logits) and float64 over the
+// steps: in fp32 alone equal logits all round the same way (rows of 2^22 of them: log probabilities off by 2e-4).  Its x are relative
+// to a logit that the largest it has seen exceeds by kRise at most, and to the largest in the end: scaled at every step
+// that rises a little, the sums would be rounded the same way as often (a rise of 0.2 over 2^22 logits: off by 2e-5).
 constexpr int kStreamSlots = 4;
+constexpr float kRise = 4.0f;
 
 template <typename T, bool WITH_T>
 __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int end, bool with_edge)
@@ -1241,6 +1243,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
     const int tid = threadIdx.x;
     Sums a;                                              // of a step, and
     double s = 0.0, t = 0.0;                             // of the steps before, both relative to a.m
+    float most_seen = -INFINITY;
     Ref ref = ref_of(a.m);
     auto rebase = [&](float m) {                         // (as `rebased`, between two steps)
         const Ref to = ref_of(m);
@@ -1271,6 +1274,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
         const int e = row.edge(tid);
         const float z = e >= 0 ? Elem<T>::load(row.p + e) : -INFINITY;
         if (z > a.m) rebase(z);
+        most_seen = z;
         if (e >= 0) add_one(z);
         end_step();
     }
@@ -1286,7 +1290,8 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
 #pragma unroll
         for (int k = 0; k < kStreamSlots; ++k) add_words<T>(v[k], most, least);
         const float m = Elem<T>::largest(most, least);
-        if (m > a.m) rebase(m);
+        most_seen = fmaxf(most_seen, m);
+        if (m > a.m + kRise) rebase(m);
 #pragma unroll
         for (int k = 0; k < kStreamSlots; ++k)
             if (i + k * 256 < end) {
@@ -1297,6 +1302,7 @@ __device__ __forceinline__ Sums stream_sums(const Span<T> &row, int begin, int e
             }
         end_step();
     }
+    if (most_seen > a.m) rebase(most_seen);
     return merge_of<64>(Sums{a.m, static_cast<float>(s), static_cast<float>(t)});
 }
 

@@ -208,3 +208,27 @@ def test_the_norm_of_equal_gradients_is_float64_rounded_once(dtype, value, size)
     v, norm = float(g[0]), torch.empty(1, device="cuda:0")
     pl.clip_gradients([g], float("inf"), norm)
     assert abs(float(norm) / (v * np.sqrt(size)) - 1.0) <= 1.001 * U, (float(norm) / (v * np.sqrt(size)) - 1.0) / U
+
+
+@pytest.mark.parametrize("dtype,V", [("fp32", 1 << 18), ("fp32", 1 << 22), ("bf16", 1 << 22)])
+def test_slowly_rising_logits_do_not_add_up_to_an_error(dtype, V):
+    """Every step of a thread meets a logit that is a little larger than all before, so that what it has is scaled again and
+    again by a factor close to 1.  The bound is that of equal logits."""
+    import torch
+    import paper_1906_08879_amd as pl
+    n, a = 64, V // 3
+    x = torch.empty((n, V), dtype=_t(dtype), device="cuda:0")
+    ramp = torch.arange(V, dtype=torch.float64, device="cuda:0") / V
+    l, H = np.zeros(n), np.zeros(n)
+    rises = (0.03, 0.2, 0.7, 1.0, 3.0, 9.0, 30.0, 100.0)
+    for k, rise in enumerate(rises):
+        x[k::len(rises)] = (rise * ramp).to(_t(dtype))
+        z = x[k].double()
+        every = z - torch.logsumexp(z, 0)
+        l[k::len(rises)], H[k::len(rises)] = float(every[a]), float(-(every.exp() * every).sum())
+    logp, ent = torch.empty(n, device="cuda:0"), torch.empty(n, device="cuda:0")
+    pl.action_logp(x, _dev(np.full(n, a, np.int32)), logp, ent)
+    tol = U * (64.0 + 4.0 * np.abs(l))
+    assert (np.abs(_host(logp) - l) <= tol).all(), (np.abs(_host(logp) - l) / tol)[:8]
+    # t is a sum of terms of up to a few units' size beside s
+    assert (np.abs(_host(ent) - H) <= 4.0 * tol).all(), (np.abs(_host(ent) - H) / tol)[:8]
