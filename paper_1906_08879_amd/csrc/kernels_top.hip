@@ -42,7 +42,7 @@ struct RowLog {
     __device__ float operator()(float z) const
     {
         const float d = z - (m == -INFINITY ? 0.0f : m);
-        if (s == 0.0f) return NAN;
+        if (!(s > 0.0f)) return NAN;                     // (nothing is allowed; a logit is no number)
         if (z == lowest && d * per2 < kNoChance) return -INFINITY;
         return d * per - log_s;
     }
