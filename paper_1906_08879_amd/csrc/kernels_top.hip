@@ -120,10 +120,10 @@ __global__ __launch_bounds__(256) void k_top_narrow(TopArgs g)
     for (int i = 0; i < g.top; ++i) {
         uint64_t best = 0;
         each([&](int j, float v) {
-            const uint64_t e = entry_of(v, j);
+            const uint64_t e = entry_of(v, j + 1);           // (from 1 on: a NaN of all bits at action 0 is below the first `before` too)
             if (e < before && e > best) best = e;
         });
-        g.out_top[n * g.top + i] = action_of(best);
+        g.out_top[n * g.top + i] = action_of(best) - 1;
         if (g.out_top_logp) g.out_top_logp[n * g.top + i] = log_p(logit_of(best));
         before = best;
     }

@@ -37,3 +37,23 @@ def test_masked_actions_of_rows_that_are_no_numbers(n, V, k, dtype):
     order = np.maximum(np.where(np.isnan(z[:3]), 0.0, _host(x)), -1e300)
     order[0, 0] = -np.inf if sign else np.inf             # a NaN below -inf, or above all; +inf first
     assert (top[:3] == np.argsort(-order, axis=1, kind="stable")[:, :k]).all()
+
+
+@pytest.mark.parametrize("n,V,k", WIDTHS + [(20, 16, 3), (20, 16, 16)])
+@pytest.mark.parametrize("bits", [0x7fffffff, 0x7fc00000, -1, -0x400000])
+def test_not_a_number_of_any_bits(n, V, k, bits):
+    """A NaN is listed once, above all others or (with its sign) below them, wherever it lies."""
+    import torch
+    import paper_1906_08879_amd as pl
+    gen = torch.Generator("cuda").manual_seed(V)
+    x = torch.randn(n, V, device="cuda:0", generator=gen)
+    at = [0, V // 2, V - 1]
+    for r, j in enumerate(at):
+        x.view(torch.int32)[r, j] = bits
+    top, lp = torch.full((n, k), -7, dtype=torch.int32, device="cuda:0"), torch.empty(n, k, device="cuda:0")
+    pl.top_actions(x, top, lp)
+    order = x.double().cpu().numpy()
+    for r, j in enumerate(at):
+        order[r, j] = np.inf if bits > 0 else -np.inf
+    assert (top.cpu().numpy() == np.argsort(-order, axis=1, kind="stable")[:, :k]).all()
+    assert torch.isnan(lp[:3]).all() and torch.isfinite(lp[3:]).all()
