@@ -512,9 +512,9 @@ int pl_top_actions(const pl_logits *logits, double temperature, int32_t n_top, i
  * (with tail, all other actions are one: the value is a divergence, >= 0 and zero where both agree), and the loss is the sum of
  * w times the value over the rows that count, w as in pl_clipped_policy_loss.  The gradient of logit j is
  *     w / T (F p_j - q_j) for listed actions,   w / T p_j (F - r / p_rest) for the others,   F = sum q + r
- * Entries whose action is outside [0, n_actions), or whose probability is zero for the teacher or the policy, are left out: with
- * tail their action is one of the others.  The rest adds nothing where r <= 0 or p_rest = 0.  An action may be listed again: its
- * entries add up.  A row without entries has value 0, with tail that of no list, 0 too, and a gradient of 0.
+ * Entries whose action is outside [0, n_actions), or whose probability is zero for the teacher or the policy (its logit is masked),
+ * are left out: with tail their action is one of the others.  The rest adds nothing where r <= 0 or all the others are masked; it counts however small
+ * p_rest is, below the smallest fp32 number too.  An action may be listed again: its entries add up.  A row without entries has value 0, with tail that of no list, 0 too, and a gradient of 0.
  *   tail         0 or 1
  *   n_top        1 .. PL_MAX_TOP (it may exceed n_actions)
  *   top          dev [n_rows, n_top] int32;  top_logp  dev [n_rows, n_top] fp32: ln q

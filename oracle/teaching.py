@@ -54,13 +54,15 @@ def distill(z, ids, lq, rows, tail=True, T=1.0, reduction="rows", n_seqs=1, grad
             values[i] += np.exp(lq[i, j]) * (lq[i, j] - every[ids[i, j]])
             coeff[i, j] = grad_scale * w[i] / T * np.exp(lq[i, j])
         mass, rest = q.sum(), p[~listed].sum()
-        r = max(0.0, 1.0 - mass) if tail and rest > 0.0 else 0.0
+        others = np.where(listed, -np.inf, every)         # in logarithms: exp(-800) is 0, what it is a part of need not be
+        log_rest = others.max() + np.log(np.exp(others - others.max()).sum()) if not np.isneginf(others).all() else -np.inf
+        r = max(0.0, 1.0 - mass) if tail and log_rest > -np.inf else 0.0
         if r > 0.0:
-            values[i] += r * (np.log(r) - np.log(rest))
+            values[i] += r * (np.log(r) - log_rest)
         F = mass + r
-        grad[i] = grad_scale * w[i] / T * np.where(listed, F * p - q, p * (F - (r / rest if r > 0.0 else 0.0)))
+        grad[i] = grad_scale * w[i] / T * np.where(listed, F * p - q, F * p - (r * np.exp(others - log_rest) if r > 0.0 else 0.0))
         stats += w[i] * np.array([values[i], mass, p[listed].sum()])
-        size[i], factor[i] = max(rest * mass, r, abs(F * rest - r)), (F, r / rest if r > 0.0 else 0.0)
+        size[i], factor[i] = max(rest * mass, r, abs(F * rest - r)), (F, r * np.exp(min(-log_rest, 700.0)) if r > 0.0 else 0.0)
     return dict(stats=stats, grad=grad, values=values, coeff=coeff, w=w, size=size, factor=factor, counts=counts)
 
 

@@ -268,6 +268,8 @@ int pl_distill_loss(const pl_logits *logits, const pl_rows *rows_in, const pl_di
     a.per = 1.0 / cfg->temperature;
     a.per2 = static_cast<float>(kLog2e / cfg->temperature);
     a.grad_scale = cfg->grad_scale;
+    // from 2^-40 on, what of a sum is below 2^-126 does not matter, and r / p_rest times the gradients' scale stays in fp32
+    if (cfg->tail) a.least = static_cast<float>(std::max(0x1p-40, std::fabs(static_cast<double>(cfg->grad_scale)) / cfg->temperature * 0x1p-124));
     a.out_grad = out_grad;
     a.grad_stride = grad_stride;
     a.out_values = out_values;

@@ -3,7 +3,10 @@
 // With x_j = (z_j - m) / T, the row's maximum m, the sum R of e^x over the actions outside the list and S = R + the sum over the
 // list: ln p_j = x_j - ln S, p_rest = R / S, and the gradient is e^{x_j} A outside the list, A = w / T (F - r / p_rest) / S.
 // R is summed over the actions outside the list themselves, which are told apart by a bit for every element: as 1 - sum p it
-// would be lost where the policy gives the list nearly everything.  What there is of a list, up to 128 entries, is done in float64 by
+// would be lost where the policy gives the list nearly everything.  Where it gives them less still, R leaves fp32 relative to the row's
+// maximum, and so does r / p_rest: rows with a tail whose R is below 2^-40 (DistillArgs::least) take it again, relative to the largest of the
+// others themselves, and their gradients too: e^{x_j} (F p_rest - r) / R with exponents that end at 0.  (A call of 512 actions a row takes 2% longer
+// for looking, where no row does.)  What there is of a list, up to 128 entries, is done in float64 by
 // one wave: values are small differences of log probabilities, and with S = R + list an error of R takes part in them only by
 // p_rest - r.  Gradients at listed actions, F p - q, are differences as well.
 //
@@ -132,10 +135,22 @@ __device__ __forceinline__ bool mark_first(List &l, int lane, int k)
     return __any(again);
 }
 
-// What follows for a row from its maximum, the sum of e^x outside the list, and the list.
+// The sum of e^x over the allowed actions outside the list (0: there are none), relative to the row's maximum or to one that is lower by
+// `down` (< 0, in units of T), `least` = e^down.
+struct Rest {
+    double sum, down, least;
+};
+
+__device__ __forceinline__ Rest rest_below(const DistillArgs &g, double sum, float m, float most)
+{
+    const double down = (static_cast<double>(most) - m) * g.per;
+    return {sum, down, exp_of(down)};
+}
+
+// What follows for a row from its maximum, its rest, and the list.
 struct RowResult {
     double value, mass, share;
-    float A;                           // e^x A: the gradient of the others
+    float A;                           // e^x A: the gradient of the others, x as in their sum
 };
 
 __device__ __forceinline__ double tail_mass(double mass, double rest, int tail)
@@ -165,17 +180,17 @@ __device__ __forceinline__ ListSums sum_list(const DistillArgs &g, List &l, int 
     return {wave_sum(s.mass), wave_sum(s.list), wave_sum(s.cross)};
 }
 
-__device__ __forceinline__ RowResult finish_list(const DistillArgs &g, List &l, int lane, const ListSums &sums, double rest, float weight, bool repeated)
+__device__ __forceinline__ RowResult finish_list(const DistillArgs &g, List &l, int lane, const ListSums &sums, const Rest &rest, float weight, bool repeated)
 {
-    const double mass = sums.mass, list = sums.list, S = rest + list;
+    const double mass = sums.mass, list = sums.list, S = fma(rest.sum, rest.least, list);
     RowResult r{0.0, mass, 0.0, 0.0f};
     if (S == 0.0) return r;                              // (nothing is allowed: nothing is listed either)
-    const double per_S = 1.0 / S, p_rest = rest * per_S, tail = tail_mass(mass, rest, g.tail), F = mass + tail;
+    const double per_S = 1.0 / S, tail = tail_mass(mass, rest.sum, g.tail), F = mass + tail, ratio = tail > 0.0 ? tail / rest.sum : 0.0;
     r.value = sums.cross + mass * log_of(S);
-    if (tail > 0.0) r.value += tail * log_of(tail / p_rest);
+    if (tail > 0.0) r.value += tail * (log_of(ratio * S) - rest.down);
     r.share = list * per_S;
     const double scale = static_cast<double>(weight) * g.grad_scale * g.per;
-    r.A = static_cast<float>(scale * (F - (tail > 0.0 ? tail / p_rest : 0.0)) * per_S);
+    r.A = static_cast<float>(scale * (F * (rest.least * per_S) - ratio));
     wave_sync();
 #pragma unroll 1
     for (int i = lane; i < g.k; i += 64) {
@@ -247,9 +262,10 @@ __device__ __forceinline__ void block_out(const DistillArgs &g, int i, double v)
     }
 }
 
-// ---- narrow rows: a row to a thread
+// ---- narrow rows: a row to a thread.  (Four waves to a SIMD: with 132 registers instead of 128, three, 200000 rows of 16 bf16 37.6 us instead
+// of 34.9.)
 template <typename T, int CAP, bool WHOLE>
-__global__ __launch_bounds__(256) void k_distill_narrow(DistillArgs g)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WHOLE ? 4 : 1))) void k_distill_narrow(DistillArgs g)
 {
     extern __shared__ float tile[];
     __shared__ double sums[4][4];
@@ -313,19 +329,32 @@ __global__ __launch_bounds__(256) void k_distill_narrow(DistillArgs g)
                 e_listed[j] = j == id ? e : e_listed[j];
             }
         }
-        float others = 0.0f;
-        each([&](int j, float v) { others += listed >> j & 1 ? 0.0f : exp2_of(x(v)); });
-        const double rest = others;
-        const double S = rest + list, per_s = S == 0.0 ? 0.0 : 1.0 / S, p_rest = rest * per_s, tail = tail_mass(mass, rest, g.tail), F = mass + tail;
+        const uint32_t others = allowed & ~listed;
+        Scale y = x;                             // of the others
+        auto e_other = [&](int j, float v) { return others >> j & 1 ? exp2_of(y(v)) : 0.0f; };
+        float sum = 0.0f;
+        each([&](int j, float v) { sum += e_other(j, v); });
+        double down = 0.0, least = 1.0;
+        if (sum < g.least && others) {
+            y.m = -INFINITY;
+            each([&](int j, float v) { y.m = others >> j & 1 ? fmaxf(y.m, v) : y.m; });
+            down = (static_cast<double>(y.m) - base) * g.per;
+            least = exp_of(down);
+            sum = 0.0f;
+            each([&](int j, float v) { sum += e_other(j, v); });
+        }
+        const double rest = sum;
+        const double S = rest * least + list, per_s = S == 0.0 ? 0.0 : 1.0 / S, tail = tail_mass(mass, rest, g.tail), F = mass + tail,
+                     ratio = tail > 0.0 ? tail / rest : 0.0;
         double value = cross + mass * log_of(S);
-        if (tail > 0.0) value += tail * log_of(tail / p_rest);
+        if (tail > 0.0) value += tail * (log_of(ratio * S) - down);
         if (S == 0.0) value = 0.0;
         const double scale = static_cast<double>(weight) * g.grad_scale * g.per;
-        const float A = S == 0.0 ? 0.0f : static_cast<float>(scale * (F - (tail > 0.0 ? tail / p_rest : 0.0)) * per_s);
+        const float A = S == 0.0 ? 0.0f : static_cast<float>(scale * (F * (least * per_s) - ratio));
         if (g.out_grad) {
             each([&](int j, float v) {
                 if (listed >> j & 1) grad[j] = static_cast<float>(scale * (F * (e_listed[j] * per_s) - q[j]));
-                else grad[j] = S == 0.0 ? 0.0f : exp2_of(x(v)) * A;
+                else grad[j] = e_other(j, v) * A;
             });
         }
         if (g.out_values) g.out_values[n] = static_cast<float>(value);
@@ -433,22 +462,42 @@ __global__ __launch_bounds__(64) void k_distill_lane(DistillArgs g)
                     if (!pass && g.out_coeff) g.out_coeff[n * g.k + i] = coeff;
                 }
                 if (pass) break;
-                double rest = 0.0;
+                Scale y = x;                         // of the others
+                double rest = 0.0, down = 0.0, least = 1.0;
+                auto sum_rest = [&]() {
+                    rest = 0.0;
 #pragma unroll 4
-                for (int j = 0; j < V; ++j) rest += bit_of(j) ? 0.0f : exp2_of(x(z[j]));
-                const double S = rest + list;
+                    for (int j = 0; j < V; ++j) rest += bit_of(j) ? 0.0f : exp2_of(y(z[j]));
+                };
+                sum_rest();
+                if (rest < g.least) {
+                    float most = -INFINITY;
+#pragma unroll 1
+                    for (int j = 0; j < V; ++j) {
+                        if (bit_of(j)) continue;
+                        if (z[j] == low && x(low) < kNoChance) z[j] = -INFINITY;
+                        most = fmaxf(most, z[j]);
+                    }
+                    if (most != -INFINITY) {
+                        y.m = most;
+                        down = (static_cast<double>(most) - base) * g.per;
+                        least = exp_of(down);
+                        sum_rest();
+                    }
+                }
+                const double S = rest * least + list;
                 per_s = S == 0.0 ? 0.0 : 1.0 / S;
                 const double p_rest = rest * per_s, tail = tail_mass(mass, rest, g.tail);
                 F = mass + tail;
                 value = cross;
 #pragma unroll 1
-                for (int l = 0; l < (tail > 0.0 ? 2 : 1); ++l) value += (l ? tail : mass) * log_of(l ? tail / p_rest : S);
+                for (int l = 0; l < (tail > 0.0 ? 2 : 1); ++l) value += (l ? tail : mass) * (log_of(l ? tail / p_rest : S) - (l ? down : 0.0));
                 if (S == 0.0) value = 0.0;
-                const float A = S == 0.0 ? 0.0f : static_cast<float>(scale * (F - (tail > 0.0 ? tail / p_rest : 0.0)) * per_s);
+                const float A = S == 0.0 ? 0.0f : static_cast<float>(scale * (F * least - (tail > 0.0 ? tail / p_rest : 0.0)) * per_s);
                 if (g.out_grad) {
 #pragma unroll 4
                     for (int j = 0; j < V; ++j)
-                        if (!bit_of(j)) z[j] = S == 0.0 ? 0.0f : exp2_of(x(z[j])) * A;
+                        if (!bit_of(j)) z[j] = S == 0.0 ? 0.0f : exp2_of(y(z[j])) * A;
                 }
             }
             if (g.out_values) g.out_values[n] = static_cast<float>(value);
@@ -528,6 +577,21 @@ __device__ __forceinline__ void write_slot(T *out, const uint4 &v, float A, cons
     stream_16(out, Elem<T>::pack(f));
 }
 
+// The elements of a slot that are masked or listed as -infinity, which has no part in a sum; and the maximum of the others.
+template <typename T>
+__device__ __forceinline__ void leave_others(uint4 &v, uint32_t marks, float masked, float &most)
+{
+    constexpr int N = Elem<T>::N;
+    float f[N];
+    Elem<T>::unpack(v, f);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        f[j] = marks >> j & 1 || f[j] == masked ? -INFINITY : f[j];
+        most = fmaxf(most, f[j]);
+    }
+    v = Elem<T>::pack(f);
+}
+
 // THREADS threads have the row in registers, CH slots each; one more wave has the list.  Its float64 arithmetic runs beside the sums,
 // and needs registers that the others hold the row in: in one of them 130 to 220 bytes a thread were spilled.
 template <typename T, int THREADS, int CH>
@@ -536,7 +600,11 @@ __global__ __launch_bounds__(THREADS + 64) __attribute__((amdgpu_waves_per_eu(4)
     constexpr int N = Elem<T>::N, WAVES = THREADS / 64;
     __shared__ Marks<THREADS, CH, N> marks;
     __shared__ List list;
-    __shared__ float most_of[WAVES], rest_of[WAVES], shared_A;
+    __shared__ float most_of[WAVES], rest_of[WAVES];
+    __shared__ struct __align__(8) {
+        float A;
+        int again;                                   // the others' sum is taken again
+    } shared;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     auto row_most = [&]() { return max_of<64>(most_of[lane < WAVES ? lane : 0]); };
@@ -569,9 +637,27 @@ __global__ __launch_bounds__(THREADS + 64) __attribute__((amdgpu_waves_per_eu(4)
             if (repeated) mark_first(list, lane, g.k);
             const ListSums sums = sum_list(g, list, lane, m);
             __syncthreads();                         // the sums of the others
-            const double rest = wave_sum(lane < WAVES ? static_cast<double>(rest_of[lane]) : 0.0);
+            auto rest_sum = [&]() { return wave_sum(lane < WAVES ? static_cast<double>(rest_of[lane]) : 0.0); };
+            Rest rest{rest_sum(), 0.0, 1.0};
+            bool given_up = g.tail && rest.sum < g.least;
+            if (given_up && g.k >= g.x.V) {          // (not where all actions are listed)
+                int listed = 0;
+                for (int i = lane; i < PL_MAX_TOP; i += 64) listed += __popcll(__ballot(i < g.k && list.first[i]));
+                given_up = listed < g.x.V;
+            }
+            if (__builtin_expect(given_up, false)) {
+                if (lane == 0) shared.again = 1;
+                __syncthreads();                     // (the others wait here for what follows from their sums)
+                __syncthreads();                     // their own maximum
+                const float most = row_most();
+                __syncthreads();                     // their sums
+                if (most != -INFINITY) rest = rest_below(g, rest_sum(), m, most);
+            }
             const RowResult r = finish_list(g, list, lane, sums, rest, weight, repeated);
-            if (lane == 0) shared_A = r.A;
+            if (lane == 0) {
+                shared.A = r.A;
+                shared.again = 0;
+            }
 #pragma unroll 1
             for (int i = lane; i < g.k; i += 64)
                 if (list.first[i]) marks.link(i, marks.next[i]);
@@ -604,7 +690,7 @@ __global__ __launch_bounds__(THREADS + 64) __attribute__((amdgpu_waves_per_eu(4)
 #pragma unroll
         for (int k = 0; k < CH; ++k)
             if (k * THREADS < whole) v[k] = row.load(k * THREADS + tid);
-        const float z_edge = edge >= 0 ? Elem<T>::load(row.p + edge) : -INFINITY;
+        float z_edge = edge >= 0 ? Elem<T>::load(row.p + edge) : -INFINITY;
         marks.clear();
         uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
 #pragma unroll
@@ -613,7 +699,7 @@ __global__ __launch_bounds__(THREADS + 64) __attribute__((amdgpu_waves_per_eu(4)
         const float wave_most = max_of<64>(fmaxf(z_edge, whole > 0 ? Elem<T>::largest(most, least) : -INFINITY));
         if (lane == 0) most_of[wave] = wave_most;
         __syncthreads();
-        const Scale x{ref_of(row_most()).m, g.per2};
+        Scale x{ref_of(row_most()).m, g.per2};
         __syncthreads();
         float rest = edge >= 0 && !marks.of_edge(tid) ? exp2_of(x(z_edge)) : 0.0f;
 #pragma unroll
@@ -629,8 +715,43 @@ __global__ __launch_bounds__(THREADS + 64) __attribute__((amdgpu_waves_per_eu(4)
         if (lane == 0) rest_of[wave] = rest;
         __syncthreads();
         __syncthreads();
+        float A = shared.A;
+        if (g.tail && __builtin_expect(shared.again, 0)) {
+            const float low = lowest_of(g.x.dtype), masked = x(low) < kNoChance ? low : -INFINITY;
+            float most = -INFINITY;
+            if (edge >= 0) {
+                if (marks.of_edge(tid) || z_edge == masked) z_edge = -INFINITY;
+                most = z_edge;
+            }
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                keep_packed(v[k]);
+                if (k * THREADS + tid < whole) leave_others<T>(v[k], marks.of_slot(k * THREADS + tid), masked, most);
+            }
+            most = max_of<64>(most);
+            if (lane == 0) most_of[wave] = most;
+            __syncthreads();
+            most = row_most();
+            if (most != -INFINITY) {                 // (else there are none, and their sum was 0)
+                x.m = most;
+                rest = edge >= 0 ? exp2_of(x(z_edge)) : 0.0f;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    keep_packed(v[k]);
+                    if (k * THREADS + tid < whole) {
+                        float f[N];
+                        Elem<T>::unpack(v[k], f);
+                        rest += unmarked_sum<N>(f, 0, x);
+                    }
+                }
+                rest = sum_of<64>(rest);
+                if (lane == 0) rest_of[wave] = rest;
+            }
+            __syncthreads();
+            __syncthreads();
+            A = shared.A;
+        }
         if (out) {
-            const float A = shared_A;
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 keep_packed(v[k]);
@@ -647,6 +768,9 @@ __global__ __launch_bounds__(THREADS + 64) __attribute__((amdgpu_waves_per_eu(4)
 // ---- rows in slices: sums over the unlisted actions, then what follows from them, then the gradient
 constexpr int kPartSlots = 8;          // of a thread in a step
 
+// Of a part's actions outside the list the sum relative to its largest logit, listed or not; where that is below `least`, or the
+// part lies near the type's lowest value, relative to their own maximum, without those at the lowest value, which are counted: whether they are masked
+// goes by the row's maximum.
 template <typename T>
 __global__ __launch_bounds__(256) void k_distill_part(DistillArgs g)
 {
@@ -661,14 +785,7 @@ __global__ __launch_bounds__(256) void k_distill_part(DistillArgs g)
         const bool with_edge = blockIdx.y == 0;
         const int edge = with_edge ? row.edge(tid) : -1;
         const float z_edge = edge >= 0 ? Elem<T>::load(row.p + edge) : -INFINITY;
-        float m = -INFINITY;
-        double s = 0.0;                              // of this thread, relative to m
-        for (int b0 = begin; b0 == begin || b0 < end; b0 += STEP) {
-            const int b1 = min(end, b0 + STEP);
-            uint4 v[kPartSlots];
-#pragma unroll
-            for (int k = 0; k < kPartSlots; ++k)
-                if (b0 + k * 256 + tid < b1) v[k] = row.load(b0 + k * 256 + tid);
+        auto set_marks = [&](int b0, int b1) {
             marks.clear();
             __syncthreads();
             for (int i = tid; i < g.k; i += 256) {
@@ -680,6 +797,16 @@ __global__ __launch_bounds__(256) void k_distill_part(DistillArgs g)
                 }
             }
             __syncthreads();
+        };
+        float m = -INFINITY;
+        double s = 0.0;                              // of this thread, relative to m
+        for (int b0 = begin; b0 == begin || b0 < end; b0 += STEP) {
+            const int b1 = min(end, b0 + STEP);
+            uint4 v[kPartSlots];
+#pragma unroll
+            for (int k = 0; k < kPartSlots; ++k)
+                if (b0 + k * 256 + tid < b1) v[k] = row.load(b0 + k * 256 + tid);
+            set_marks(b0, b1);
             uint32_t most = Elem<T>::kNone, least = 0xffffffffu;
 #pragma unroll
             for (int k = 0; k < kPartSlots; ++k)
@@ -704,13 +831,47 @@ __global__ __launch_bounds__(256) void k_distill_part(DistillArgs g)
         s = wave_sum(s == 0.0 ? 0.0 : s * exp2_of((m - ref_of(wave_m).m) * g.per2));
         if (lane == 0) part[wave] = {wave_m, static_cast<float>(s), 0.0f};
         __syncthreads();
-        if (tid == 0) {
-            const float all = fmaxf(fmaxf(part[0].m, part[1].m), fmaxf(part[2].m, part[3].m));
-            double sum = 0.0;
-            for (int w = 0; w < 4; ++w)
-                if (part[w].s != 0.0f) sum += static_cast<double>(part[w].s) * exp2_of((part[w].m - ref_of(all).m) * g.per2);
-            g.parts[n * g.slices + blockIdx.y] = {all, static_cast<float>(sum), 0.0f};
+        const float all = fmaxf(fmaxf(part[0].m, part[1].m), fmaxf(part[2].m, part[3].m)), low = lowest_of(g.x.dtype);
+        double sum = 0.0;
+        for (int w = 0; w < 4; ++w)
+            if (part[w].s != 0.0f) sum += static_cast<double>(part[w].s) * exp2_of((part[w].m - ref_of(all).m) * g.per2);
+        DistillPart of{all, all, static_cast<float>(sum), 0.0f};
+        if (g.tail && all != -INFINITY && (sum < g.least || !((low - all) * g.per2 < kNoChance))) {
+            of.base = -INFINITY;
+            of.s = 0.0f;
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {   // the maximum and the number of the lowest; the sum
+                const Scale x{ref_of(of.base).m, g.per2};
+                float most = -INFINITY, add = 0.0f;
+                auto take = [&](float z) {
+                    if (z != low) most = fmaxf(most, z);
+                    add += pass ? (z == low ? 0.0f : exp2_of(x(z))) : z == low ? 1.0f : 0.0f;
+                };
+#pragma unroll 1
+                for (int b0 = begin; b0 == begin || b0 < end; b0 += STEP) {
+                    const int b1 = min(end, b0 + STEP);
+                    __syncthreads();
+                    set_marks(b0, b1);
+                    if (b0 == begin && edge >= 0 && !marks.of_edge(tid)) take(z_edge);
+#pragma unroll 2
+                    for (int i = b0 + tid; i < b1; i += 256) {
+                        float f[N];
+                        Elem<T>::unpack(row.load(i), f);
+                        const uint32_t marked = marks.of_slot(i - b0);
+#pragma unroll
+                        for (int j = 0; j < N; ++j)
+                            if (!(marked >> j & 1)) take(f[j]);
+                    }
+                }
+                most = max_of<64>(most);
+                add = sum_of<64>(add);
+                if (lane == 0) part[wave] = {most, add, 0.0f};
+                __syncthreads();
+                of.base = fmaxf(fmaxf(part[0].m, part[1].m), fmaxf(part[2].m, part[3].m));
+                (pass ? of.s : of.lowest) = (part[0].s + part[1].s) + (part[2].s + part[3].s);
+            }
         }
+        if (tid == 0) g.parts[n * g.slices + blockIdx.y] = of;
         __syncthreads();
     }
 }
@@ -733,18 +894,37 @@ __global__ __launch_bounds__(256) void k_distill_finish(DistillArgs g)
             for (int i = lane; i < g.slices; i += 64) m = fmaxf(m, g.parts[n * g.slices + i].m);
             read_logits<T>(read, g, n);
             m = max_of<64>(m);
-            double rest = 0.0;
-            for (int i = lane; i < g.slices; i += 64) {
-                const RowPart of = g.parts[n * g.slices + i];
-                if (of.s != 0.0f) rest += static_cast<double>(of.s) * exp2_of((of.m - ref_of(m).m) * g.per2);
+            // the sum of the others relative to `to`
+            const float low = lowest_of(g.x.dtype);
+            auto sum_rest = [&](float to, bool with_lowest) {
+                const Scale x{ref_of(to).m, g.per2};
+                double sum = 0.0;
+                for (int i = lane; i < g.slices; i += 64) {
+                    const DistillPart of = g.parts[n * g.slices + i];
+                    if (of.s != 0.0f) sum += static_cast<double>(of.s) * exp2_of(x(of.base));
+                    if (of.lowest != 0.0f && with_lowest) sum += static_cast<double>(of.lowest) * exp2_of(x(low));
+                }
+                return wave_sum(sum);
+            };
+            Rest rest{sum_rest(m, true), 0.0, 1.0};
+            float base = m;
+            const bool given_up = rest.sum < g.least, masked = Scale{ref_of(m).m, g.per2}(low) < kNoChance;
+            if (given_up) {
+                float most = -INFINITY;
+                for (int i = lane; i < g.slices; i += 64) {
+                    const DistillPart of = g.parts[n * g.slices + i];
+                    if (of.s != 0.0f) most = fmaxf(most, of.base);
+                    if (of.lowest != 0.0f && !masked) most = fmaxf(most, low);
+                }
+                most = max_of<64>(most);
+                if (most != -INFINITY) rest = rest_below(g, sum_rest(base = most, !masked), m, most);
             }
-            rest = wave_sum(rest);
             keep_list(list, read, m, g, lane);
             const bool repeated = mark_first(list, lane, g.k);
             const float weight = weight_of(g, place.seq);
             const RowResult r = finish_list(g, list, lane, sum_list(g, list, lane, m), rest, weight, repeated);
             row_outputs(g, n, lane, list, r, weight, acc);
-            rg = {m, r.A, 0.0f, 0.0f};
+            rg = {base, r.A, given_up && masked ? 1.0f : 0.0f, 0.0f};
         } else {
             row_nothing(g, n, lane);
         }
@@ -784,7 +964,15 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs g, int chunks)
 #pragma unroll
         for (int k = 0; k < kGradChunk; ++k)
             if (b0 + k * 256 + tid < b1) v[k] = row.load(b0 + k * 256 + tid);
-        const float z_edge = edge >= 0 ? Elem<T>::load(row.p + edge) : 0.0f;
+        float z_edge = edge >= 0 ? Elem<T>::load(row.p + edge) : 0.0f;
+        if (rg.B != 0.0f) {                          // (actions at the lowest value are masked)
+            const float low = lowest_of(g.x.dtype);
+            float most = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kGradChunk; ++k)
+                if (b0 + k * 256 + tid < b1) leave_others<T>(v[k], 0, low, most);
+            if (z_edge == low) z_edge = -INFINITY;
+        }
         marks.head[tid] = -1;
         __syncthreads();
         if (tid < g.k) {
@@ -827,7 +1015,9 @@ DistillWorkspace carve_distill_workspace(void *base, const LogitsView &x, const 
     DistillWorkspace w;
     w.loss = carve_loss_workspace(base, x, rows);
     size_t pos = (w.loss.bytes + 15) / 16 * 16;
-    const size_t n = in_slices(x) ? static_cast<size_t>(x.n) * k : 0;
+    const size_t n = in_slices(x) ? static_cast<size_t>(x.n) * k : 0, parts = in_slices(x) ? static_cast<size_t>(x.n) * w.loss.slices : 0;
+    w.parts = base ? reinterpret_cast<DistillPart *>(static_cast<char *>(base) + pos) : nullptr;
+    pos += parts * sizeof(DistillPart);
     w.at = base ? reinterpret_cast<int32_t *>(static_cast<char *>(base) + pos) : nullptr;
     pos += (n * 4 + 15) / 16 * 16;
     w.inside = base ? reinterpret_cast<float *>(static_cast<char *>(base) + pos) : nullptr;
@@ -879,7 +1069,7 @@ void launch_distill(DistillArgs a, int reduction, const DistillWorkspace &ws, hi
                 else over_rows(k_distill_row<T, 960, 18>, 1024);
                 return;
             }
-            a.parts = ws.loss.parts;
+            a.parts = ws.parts;
             a.slices = ws.loss.slices;
             a.row_grad = ws.loss.grad;
             a.at = ws.at;

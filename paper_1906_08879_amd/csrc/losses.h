@@ -126,6 +126,12 @@ struct TopWorkspace {
 TopWorkspace carve_top_workspace(void *base, const LogitsView &x, int top);
 void launch_top(TopArgs a, const TopWorkspace &ws, hipStream_t s);
 
+// A part of a row: its largest logit; of its actions outside the list the sum s of e^{(z - base) / T}, and the number of those at the lowest
+// value that are not in it.
+struct DistillPart {
+    float m, base, s, lowest;
+};
+
 struct DistillArgs {
     LogitsView x;
     RowsView rows;
@@ -135,21 +141,23 @@ struct DistillArgs {
     int k, tail;
     double per;                        // 1 / T
     float per2, grad_scale;
+    float least;                       // sums over the unlisted actions below it are taken again relative to their own maximum; 0 without tail
     void *out_grad;
     int64_t grad_stride;
     float *out_values, *out_coeff;
     double *sums;                      // [workgroups, 4]
     float *out_stats;
     uint32_t magic;
-    RowPart *parts;                    // rows in slices
+    DistillPart *parts;                // [n, slices], rows in slices
     int slices;
-    RowGrad *row_grad;                 // [n], and what their gradients are at the listed actions
+    RowGrad *row_grad;                 // [n] (B: whether actions at the lowest value are masked), and what the gradients at the listed actions are
     int32_t *at;                       // [n, k] action, or -1
     float *inside;                     // [n, k]
 };
 
 struct DistillWorkspace {
     LossWorkspace loss;
+    DistillPart *parts = nullptr;
     int32_t *at = nullptr;
     float *inside = nullptr;
     double *sums = nullptr;            // [workgroups, 4]
