@@ -835,8 +835,12 @@ def orthogonal_update(grads, momentum=None, out_momentum=None, weights=None, out
     scales = [float(scales)] * n if isinstance(scales, (int, float)) else [float(s) for s in scales]
     if len(scales) != n:
         raise PlacetoError(f"scales has {len(scales)} numbers, grads {n} tensors")
-    factors = array("f", [float(f) for step in iteration for f in step])
-    if any(len(step) != 3 for step in iteration):
+    try:
+        steps = [tuple(step) for step in iteration]
+        factors = array("f", [float(f) for step in steps for f in step])
+    except (TypeError, ValueError):
+        steps = [()]
+    if any(len(step) != 3 for step in steps):
         raise PlacetoError("iteration must be (a, b, c) of every step")
     views = (MatrixView * max(1, n))()
     for i, g in enumerate(grads):
