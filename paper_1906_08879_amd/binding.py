@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 from array import array
+from numbers import Real
 from typing import Optional
 
 import numpy as np
@@ -832,7 +833,10 @@ def orthogonal_update(grads, momentum=None, out_momentum=None, weights=None, out
     new_w_at = w_at if out_weights is None else _matrix_views(out_weights, grads, None, "out_weights")
     out = None if out is None else list(out)
     out_at = none if out is None else _matrix_views(out, grads, None, "out")
-    scales = [float(scales)] * n if isinstance(scales, (int, float)) else [float(s) for s in scales]
+    try:
+        scales = [float(scales)] * n if isinstance(scales, (int, float, Real)) else [float(s) for s in scales]
+    except (TypeError, ValueError):
+        raise PlacetoError("scales must be a number, or one for every tensor of grads") from None
     if len(scales) != n:
         raise PlacetoError(f"scales has {len(scales)} numbers, grads {n} tensors")
     try:

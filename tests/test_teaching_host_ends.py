@@ -20,3 +20,11 @@ def test_iterations_that_can_be_read_once(lib):  # noqa: F811
         if isinstance(bad, list):
             with pytest.raises(pl.PlacetoError):
                 pl.orthogonal_update([], out=[], iteration=(step for step in bad))
+
+
+def test_scales_of_other_types(lib):  # noqa: F811
+    for scales in (2, 0.5, np.float32(0.5), np.float64(0.5), np.int64(2), [], (), np.zeros(0)):
+        pl.orthogonal_update([], out=[], scales=scales)
+    for bad in (None, "1", ["a"], [1.0], np.array(0.5), np.float32([0.5]), object()):
+        with pytest.raises(pl.PlacetoError):
+            pl.orthogonal_update([], out=[], scales=bad)
