@@ -573,8 +573,10 @@ int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clippe
  *   iteration    host [n_steps, 3]: a, b, c of every step.  Refused where a singular value of 1 and below could make
  *                the largest one, or a + b s^2 + c s^4, leave 2^-20 .. 2^20 after a step
  *   n_matrices   0 .. 2^16 (0: nothing is done)
- * All arrays but those two are device memory; the host arrays are read before the call returns.  Workspace (about 12 bytes for an
- * element and 8 for one of the square of the shorter side, and sums that workgroups share), stream and capture as above. */
+ * All arrays but those two are device memory; the host arrays are read before the call returns.  Stream and capture as above, workspace
+ * too.  Its bytes: for a matrix of sides k <= n of up to 16 x 4096, 32 x 2048 or 64 x 1024 between 32 and 256 KiB.  For others, with k' and n' the next
+ * multiples of 32, 4 k n' + 8 n k' + 8 k k' (12 an element and 8 one of k x k; 268 an element where k is 1), and where few tiles of 64 x 64
+ * of X X' are shared by workgroups, 16 KiB for each of those and up to every 256 elements of n.  Up to 16 KiB a matrix for sums and lists. */
 typedef struct {
     int32_t rows, cols;
     int32_t grad_dtype, weight_dtype, out_dtype;

@@ -28,3 +28,20 @@ def test_scales_of_other_types(lib):  # noqa: F811
     for bad in (None, "1", ["a"], [1.0], np.array(0.5), np.float32([0.5]), object()):
         with pytest.raises(pl.PlacetoError):
             pl.orthogonal_update([], out=[], scales=bad)
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (1, 4096), (1, 4097), (1, 1 << 21), (4097, 1), (8, 50000), (5, 6000), (17, 2049), (33, 1024), (33, 1025), (64, 1024), (65, 64),
+                                   (65, 1024), (333, 1111), (1000, 3000), (1024, 1024), (4096, 4096), (3000, 100000)])
+def test_workspace_is_as_large_as_documented(lib, shape):  # noqa: F811
+    """Sides padded to 32 count for thin matrices; small ones have rooms of a few sizes."""
+    k, n = min(shape), max(shape)
+    k32, n32, tiles = -(-k // 32) * 32, -(-n // 32) * 32, -(-k // 64)
+    size = pl.orthogonal_workspace_bytes([shape])
+    if n <= (4096 if k <= 16 else 2048 if k <= 32 else 1024) and k <= 64:
+        least, most = 32 << 10, 256 << 10
+    else:
+        least = 4 * k * n32 + 8 * n * k32 + 8 * k * k32
+        most = least + tiles * (tiles + 1) // 2 * -(-n // 256) * (16 << 10)
+    assert least <= size <= most + (16 << 10)
+    assert size == pl.orthogonal_workspace_bytes([shape[::-1]])
+    assert pl.orthogonal_workspace_bytes([shape] * 5) <= 5 * (most + (16 << 10))
