@@ -183,3 +183,15 @@ def test_in_place_where_the_rest_is_given_up(n, V):
     pl.distill_loss(x, _dev(ids), _dev(lq), stats[0], out_grad=out)
     pl.distill_loss(x, _dev(ids), _dev(lq), stats[1], out_grad=x)
     assert torch.equal(x, out) and torch.equal(stats[0], stats[1])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("gap", [0.0, 120.0])
+def test_the_largest_number_of_actions(gap, dtype):
+    rng = np.random.default_rng(24)
+    z, ids, lq = _given_up(rng, 1, 1 << 24, dtype, (gap,), 1.0)
+    z[0, ids[0]] = 0.0
+    ids[0, :2] = [(1 << 24) - 1, 0]
+    z[0, ids[0]] = 3.0 + gap
+    run(_round(z, dtype), ids, lq, dtype, grad_scale=1024.0)
+    run(_round(z, dtype), ids, lq, dtype, grad_scale=1024.0, offset=1)

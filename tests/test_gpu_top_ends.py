@@ -57,3 +57,14 @@ def test_not_a_number_of_any_bits(n, V, k, bits):
         order[r, j] = np.inf if bits > 0 else -np.inf
     assert (top.cpu().numpy() == np.argsort(-order, axis=1, kind="stable")[:, :k]).all()
     assert torch.isnan(lp[:3]).all() and torch.isfinite(lp[3:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_the_largest_number_of_actions(dtype):
+    """2^24 actions: hundreds of slices, indexes of 24 bits, equal logits at both ends."""
+    from tests.test_gpu_top import _check, _round
+    rng = np.random.default_rng(24)
+    z = _round(rng.normal(0, 3, (1, 1 << 24)), dtype)
+    _check(z, 128, dtype, rng)
+    z[0, [0, 1, 77, (1 << 24) - 2, (1 << 24) - 1]] = 40.0
+    _check(z, 20, dtype, rng, pad=1, offset=1)
