@@ -560,10 +560,10 @@ int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clippe
  *     out = X;     weight' = (1 - lr decay) weight - lr scale X
  * With the usual factors (3.4445, -4.7750, 2.0315), five times, the singular values of X end in about 0.7 .. 1.2.
  *
- * Numbers: the norm is summed in float64; the products' operands are kept in 22 bits below each matrix' largest possible element
- * and multiplied as three products of fp16 with fp32 sums: factors of normal matrices are off by 0.8 to 4e-6 of their norm.  That is
- * 0.5 to 0.9 times what fp32 products leave where the shorter side is above 256, up to 1.4 times where such a matrix is nearly of low rank, and up to 2.6 times with
- * few rows (5 x 94).  Momentum is fp32; outputs are rounded once to their types.  A matrix of zeros gives X = 0; one whose norm is NaN or infinite gives NaN everywhere.
+ * Numbers: the norm is summed in float64.  Up to 32 rows (or columns) all products are float64.  With more, the products' operands are kept in 22 bits below
+ * each matrix' largest possible element and multiplied as three products of fp16 with fp32 sums: factors of normal matrices are off by 0.8 to 4e-6 of their
+ * norm, 0.5 to 0.9 times what fp32 products leave where the shorter side is above 256, up to 1.4 times with fewer rows or where a matrix is nearly of low
+ * rank.  Momentum is fp32; outputs are rounded once to their types.  A matrix of zeros gives X = 0; one whose norm is NaN or infinite gives NaN everywhere.
  * Summation orders are fixed by the sizes of a call's matrices: equal calls give equal bits, but a matrix' last bits may go by the others.
  *
  *   matrices     host [n_matrices].  rows, cols 1 .. 2^21 with rows cols < 2^31; rows of every array lie `.._stride` elements apart
@@ -575,9 +575,9 @@ int pl_clip_gradients(int32_t n_tensors, void *const *grads, void *const *clippe
  *                the largest one, or a + b s^2 + c s^4, leave 2^-20 .. 2^20 after a step
  *   n_matrices   0 .. 2^16 (0: nothing is done)
  * All arrays but those two are device memory; the host arrays are read before the call returns.  Stream and capture as above, workspace
- * too.  Its bytes: for a matrix of sides k <= n of up to 16 x 4096, 32 x 2048 or 64 x 1024 between 32 and 256 KiB.  For others, with k' and n' the next
- * multiples of 32, 4 k n' + 8 n k' + 8 k k' (12 an element and 8 one of k x k; 268 an element where k is 1), and where few tiles of 64 x 64
- * of X X' are shared by workgroups, 16 KiB for each of those and up to every 256 elements of n.  Up to 16 KiB a matrix for sums and lists. */
+ * too.  Its bytes: for a matrix of sides k <= n, k up to 32, none up to 16 x 4096 or 32 x 2048 and at most 2 MiB beyond; with k up to 64 and n up to
+ * 1024 between 32 and 256 KiB; for others, with k' and n' the next multiples of 32, 4 k n' + 8 n k' + 8 k k' (12 an element and 8 one of k x k), and where few
+ * tiles of 64 x 64 of X X' are shared by workgroups, 16 KiB for each of those and up to every 256 elements of n.  Up to 16 KiB a matrix for sums and lists. */
 typedef struct {
     int32_t rows, cols;
     int32_t grad_dtype, weight_dtype, out_dtype;

@@ -27,7 +27,10 @@ _NO_STRUCTURE = ["-mllvm", "-structurizecfg-skip-uniform-regions"]
 # The float64 constants of exp and log are not taken out of the loops over rows, where they would be held (and spilled, 53 scalar
 # registers of them) beside the rows: 117 vector registers without a row in them, 93 so.
 _NO_HOIST = ["-mllvm", "-disable-machine-licm"]
-SOURCE_FLAGS = {"kernels_distill.hip": _NO_HOIST, "kernels_simulator.hip": _NO_STRUCTURE, "kernels_mfma.hip": _NO_STRUCTURE, "kernels_tiles.hip": _NO_STRUCTURE, "kernels_wide.hip": _NO_STRUCTURE, "kernels_lanes.hip": _NO_STRUCTURE}
+# A table of matrices that is passed by value is read where the caller put it only if the compiler has looked at all of its uses (300 as a
+# rule); else every workgroup copies its 3.5 KB to memory first.
+_ALL_USES = ["-mllvm", "-instcombine-max-copied-from-constant-users=100000"]
+SOURCE_FLAGS = {"kernels_distill.hip": _NO_HOIST, "kernels_orthogonal_small.hip": _ALL_USES, "kernels_simulator.hip": _NO_STRUCTURE, "kernels_mfma.hip": _NO_STRUCTURE, "kernels_tiles.hip": _NO_STRUCTURE, "kernels_wide.hip": _NO_STRUCTURE, "kernels_lanes.hip": _NO_STRUCTURE}
 
 
 def hipcc() -> str:

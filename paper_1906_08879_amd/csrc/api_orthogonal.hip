@@ -173,25 +173,35 @@ OrthMatrix place_matrix(const pl_matrix &m, Carver *c, OrthGrid *g)
     return o;
 }
 
-bool is_small(const pl_matrix &m) { return orth_small(std::min(m.rows, m.cols), std::max(m.rows, m.cols)); }
+int shorter(const pl_matrix &m) { return std::min(m.rows, m.cols); }
+int longer(const pl_matrix &m) { return std::max(m.rows, m.cols); }
 
-int32_t count_small(int32_t n_matrices, const pl_matrix *matrices)
+enum Class { SMALL, LONG, LARGE };     // a workgroup each; of few rows, in parts; in tiles
+
+Class class_of(const pl_matrix &m)
 {
-    return static_cast<int32_t>(std::count_if(matrices, matrices + n_matrices, is_small));
+    return orth_small(shorter(m), longer(m)) ? SMALL : orth_long(shorter(m), longer(m)) ? LONG : LARGE;
 }
 
-// The matrices that are not small, those with the longest sums first (workgroups begin in that order): f(matrix).
+int32_t count_of(int32_t n_matrices, const pl_matrix *matrices, Class what)
+{
+    return static_cast<int32_t>(std::count_if(matrices, matrices + n_matrices, [&](const pl_matrix &m) { return class_of(m) == what; }));
+}
+
+// The large matrices, those with the longest sums first (workgroups begin in that order): f(matrix).
 template <typename F>
 void each_large(int32_t n_matrices, const pl_matrix *matrices, F f)
 {
     for (int bit = 31; bit >= 0; --bit)
         for (int32_t i = 0; i < n_matrices; ++i)
-            if (!is_small(matrices[i]) && std::max(matrices[i].rows, matrices[i].cols) >> bit == 1) f(matrices[i]);
+            if (class_of(matrices[i]) == LARGE && longer(matrices[i]) >> bit == 1) f(matrices[i]);
 }
+
+constexpr int64_t kMostWorkgroups = 1 << 22;     // (of 512 threads, 2^32 together at most)
 
 bool fits(const OrthGrid &g)
 {
-    const int64_t most = 1 << 22;                // workgroups (of 512 threads, 2^32 together at most)
+    const int64_t most = kMostWorkgroups;
     return g.sums <= most && g.layouts <= most && g.work[0].tiles <= most && g.work[2].tiles <= most;
 }
 
@@ -206,8 +216,8 @@ void choose_work(int32_t n_matrices, const pl_matrix *matrices, int product, Ort
         const OrthKind &t = kOrthKinds[kind];
         double count = 0.0, work = 0.0, longest = 0.0;
         for (int32_t i = 0; i < n_matrices; ++i) {
-            if (is_small(matrices[i])) continue;
-            const int k = std::min(matrices[i].rows, matrices[i].cols), n = std::max(matrices[i].rows, matrices[i].cols);
+            if (class_of(matrices[i]) != LARGE) continue;
+            const int k = shorter(matrices[i]), n = longer(matrices[i]);
             const int blocks = tiles(product == 0 ? n : k, kOrthBlock), parts = tiles(blocks, part_blocks);
             const double depth = std::min(blocks, part_blocks) + kBegin, of_it = static_cast<double>(product_tiles(k, n, product, t.tile)) * parts;
             count += of_it;
@@ -227,7 +237,7 @@ void choose_work(int32_t n_matrices, const pl_matrix *matrices, int product, Ort
         for (int blocks = 8; blocks <= 64; blocks += blocks < 16 ? 4 : blocks < 32 ? 8 : 16) consider(0, blocks);
 }
 
-// The room and the launches of the matrices that are not small; false: too many of them.
+// The room and the launches of the large matrices; false: too many of them.
 bool plan_large(int32_t n_matrices, const pl_matrix *matrices, Carver *c, OrthGrid *g, OrthMatrix **list)
 {
     for (int p = 0; p < 3; ++p) choose_work(n_matrices, matrices, p, &g->work[p]);
@@ -255,12 +265,18 @@ size_t pl_orthogonal_workspace(int32_t n_matrices, const pl_matrix *matrices)
     Carver c{nullptr};
     OrthGrid g{};
     OrthMatrix *list;
+    int64_t parts = 0;
     for (int32_t i = 0; i < n_matrices; ++i) {
         if (check_size(matrices[i])) return 0;
-        if (is_small(matrices[i])) c.take<float>(orth_room(matrices[i].rows, matrices[i].cols));
+        const Class what = class_of(matrices[i]);
+        if (what != LARGE) c.take<char>(orth_room(matrices[i].rows, matrices[i].cols));
+        if (what == LONG) parts += orth_parts(longer(matrices[i]));
     }
-    const int32_t n_small = count_small(n_matrices, matrices);
-    if (n_small > kOrthSmallListed) c.take<OrthSmall>(n_small);
+    if (parts > kMostWorkgroups) return 0;
+    for (const Class what : {SMALL, LONG}) {
+        const int32_t n = count_of(n_matrices, matrices, what);
+        if (n > kOrthSmallListed) c.take<OrthSmall>(n);
+    }
     return plan_large(n_matrices, matrices, &c, &g, &list) ? c.pos : 0;
 }
 
@@ -288,45 +304,40 @@ int pl_orthogonal_update(int32_t n_matrices, const pl_matrix *matrices, const pl
 
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const OrthCfg c{static_cast<float>(1.0 - static_cast<double>(cfg->lr) * cfg->decay), cfg->lr, cfg->beta, cfg->eps, cfg->nesterov};
-    // small ones a workgroup each
+    // those of few rows
     OrthSmallTable small;
     std::copy(steps, steps + cfg->n_steps, small.step);
+    std::copy(cfg->iteration, cfg->iteration + 3 * cfg->n_steps, &small.iteration[0][0]);
     small.cfg = c;
     small.x_scale = x_scale;
     small.per_last = 1.0f / last_scale;
     small.n_steps = cfg->n_steps;
-    small.n = 0;
     Carver carver{static_cast<char *>(workspace)};
-    const int32_t n_small = count_small(n_matrices, matrices);
-    OrthSmall *small_list = n_small > kOrthSmallListed ? carver.take<OrthSmall>(n_small) : nullptr;
-    int32_t small_listed = 0;
-    for (int shape = 0; shape < 3; ++shape) {        // up to 64 x 1024 together, then longer ones of up to 16 rows, of up to 32
-        const int32_t first = small_listed;
-        int k = 0, n = 0;
-        const auto flush = [&]() {
-            if (small_list && small.n) launch_orth_small_list(small, small_list, small_listed, s);
-            small_listed += small.n;
-            if (small_list) small.n = 0;
-        };
+    for (const Class what : {SMALL, LONG}) {
+        const int32_t count = count_of(n_matrices, matrices, what);
+        if (count == 0) continue;
+        OrthSmall *small_list = count > kOrthSmallListed ? carver.take<OrthSmall>(count) : nullptr;
+        int32_t listed = 0, parts = 0;
+        small.n = 0;
         for (int32_t i = 0; i < n_matrices; ++i) {
             const pl_matrix &m = matrices[i];
-            const int shorter = std::min(m.rows, m.cols), longer = std::max(m.rows, m.cols);
-            if (!is_small(m) || shape != (longer <= kOrthSmall / 64 ? 0 : shorter <= 16 ? 1 : 2)) continue;
-            k = std::max(k, shorter);
-            n = std::max(n, longer);
+            if (class_of(m) != what) continue;
             const auto u32 = [](int64_t v) { return static_cast<uint32_t>(v); };
             const auto u8 = [](int32_t v) { return static_cast<uint8_t>(v); };
             small.m[small.n++] = {m.grad, m.weight, m.momentum, m.new_momentum, m.new_weight, m.out,
-                                  carver.take<float>(orth_room(m.rows, m.cols)),
+                                  carver.take<char>(orth_room(m.rows, m.cols)),
                                   u32(m.grad_stride), u32(m.momentum_stride), u32(m.new_momentum_stride), u32(m.weight_stride),
-                                  u32(m.new_weight_stride), u32(m.out_stride), static_cast<uint16_t>(m.rows), static_cast<uint16_t>(m.cols),
+                                  u32(m.new_weight_stride), u32(m.out_stride), m.rows, m.cols, parts,
                                   u8(m.grad_dtype), u8(m.weight_dtype), u8(m.out_dtype), m.scale};
-            if (small_list && small.n == kOrthSmallListed) flush();
+            if (what == LONG) parts += orth_parts(longer(m));
+            if (small_list && (small.n == kOrthSmallListed || listed + small.n == count)) {
+                launch_orth_small_list(small, small_list, listed, s);
+                listed += small.n;
+                small.n = 0;
+            }
         }
-        flush();
-        if (small_listed > first)
-            launch_orth_small(small, small_list ? small_list + first : nullptr, small_listed - first, k, n, s);
-        small.n = 0;
+        if (what == SMALL) launch_orth_small(small, small_list, count, s);
+        else launch_orth_long(small, small_list, count, parts, s);
     }
     OrthGrid grid{};
     OrthMatrix *list;

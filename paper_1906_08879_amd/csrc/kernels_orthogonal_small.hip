@@ -1,6 +1,15 @@
-// The orthogonalised update of small matrices (include/placeto.h): everything in one workgroup, one launch for many matrices.
+// The orthogonalised update of matrices of few rows (include/placeto.h): everything in one workgroup, one launch for many matrices; long ones
+// of up to 32 rows in parts.
 //
-// X, at most 64 rows and 1024 columns, 32 and 2048 or 16 and 4096, lies in registers: a wave has 16 NB columns as 16 x 16 parts, of
+// Up to 32 rows the iteration goes over the short side alone, in float64: with A_0 = X X', step i has B_i = a I + b A_i + c A_i^2 and
+// A_{i+1} = B_i A_i B_i, and X ends as (B_n .. B_1) X.  All of them are polynomials of A_0, symmetric, and trade places in a product.  X is read twice,
+// once for A_0 and once for the result, whatever the number of steps.  In float64 nothing is lost by it (the factors' product has entries up to 485 beside
+// results of 1, which fp32 would leave with 10^-4 of nearly dependent rows): results are off by their last rounding, 3e-8 of the factor's
+// norm, where fp32 products leave 1e-6 and products of two halves (kernels_orthogonal.hip) up to 2.9e-6 with few rows.  Bound by the two products with X on
+// the float64 matrix cores (64 multiply-adds a cycle of a CU) and, in between, by the latency of three short products a step: 16 x 4096 takes 38 us (in
+// halves, step by step, 104), 32 x 2048 49 (116); in parts 32 x 100000 45 (531) and 32 x 1048576 122 (1692), 3.3 TB/s.
+//
+// With 33 to 64 rows, and up to 1024 columns, X lies in registers: a wave has 16 NB columns as 16 x 16 parts, of
 // which a lane holds column lane % 16, rows 4 (lane / 16) .. + 3, in the two halves that kernels_orthogonal.hip explains.  That is both
 // what a product on the matrix cores (16 x 16 x 16) leaves and what the next one takes as its right operand: B X needs no movement of X.  X X' takes X as both operands
 // along the columns, that is the parts transposed: fed as a left operand and multiplied by the unit matrix, a part comes out
@@ -8,12 +17,10 @@
 //
 // Bound by the conversions between the two halves and fp32, beside the products, of the matrix with the most columns: the 24 matrices
 // of a policy network, up to 896 x 64, take 115 us in one launch, five iterations of 21 us; in tiles of several workgroups an iteration of
-// 65 rows and more is three launches one behind another, of 9 to 14 us each.  16 x 4096 104 us, 32 x 2048
-// 116 us; two of 34 x 1662, in tiles, 118 us.
+// 65 rows and more is three launches one behind another, of 9 to 14 us each.
 #include <algorithm>
 
-#include "elements.h"
-#include "orthogonal.h"
+#include "orthogonal_device.h"
 
 namespace pl {
 namespace {
@@ -39,14 +46,6 @@ struct Group {
         *reinterpret_cast<vector *>(static_cast<T *>(p) + i) = x;
     }
 };
-
-template <typename F>
-__device__ __forceinline__ void for_type(int dtype, F f)
-{
-    if (dtype == PL_F32) f(float{});
-    else if (dtype == PL_BF16) f(__bf16{});
-    else f(_Float16{});
-}
 
 struct Part {                          // of a matrix, 16 x 16
     half4 hi, lo;
@@ -91,8 +90,9 @@ __device__ __forceinline__ float4_t product(const Part &a, const Part &a2, const
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(beside(a.lo, a2.lo), bh, c, 0, 0, 0);
 }
 
+constexpr int KB = 4;                  // parts of the rows: 33 to 64 of them
+
 // Symmetric matrices in LDS, 16 KB rows of both halves; rows are an odd number of 8-byte words apart.
-template <int KB>
 struct Square {
     static constexpr int K = KB * 16, PITCH = K + 4;
     _Float16 hi[K][PITCH], lo[K][PITCH];
@@ -120,26 +120,25 @@ struct Square {
 constexpr int kWaves = 8;
 constexpr int kGroups = 8;             // of a matrix' elements that a thread has on their way at a time
 
-template <int KB>
 struct SmallShared {
     static constexpr int PAIRS = KB * (KB + 1) / 2;
-    Square<KB> A, B;
+    Square A, B;
     float4_t added[kWaves / 2][PAIRS][64];
     double sums[kWaves];
 };
 
-template <int KB, int NB>
-__device__ __forceinline__ void update_small(const OrthSmallTable &t, const OrthSmall &o, SmallShared<KB> &sh)
+template <int NB>
+__device__ __forceinline__ void update_small(const OrthSmallTable &t, const OrthSmall &o, SmallShared &sh)
 {
-    constexpr int PAIRS = SmallShared<KB>::PAIRS;
-    Square<KB> &A = sh.A, &B = sh.B;
+    constexpr int PAIRS = SmallShared::PAIRS;
+    Square &A = sh.A, &B = sh.B;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool tall = o.rows > o.cols;
     const int quad = lane >> 4;
     // Momentum and direction, in the order of the matrix, and from there to the parts through memory (fp32, columns of X one behind
     // another, with zeros to whole parts): a loop over elements for every type, instead of every type in code that is unrolled
     // over the parts.
-    float *u = o.room;
+    float *u = static_cast<float *>(o.room);
     constexpr int pitch = KB * 16;
     for (int i = tid; i < kWaves * NB * 4 * pitch; i += kWaves * 64) reinterpret_cast<float4_t *>(u)[i] = float4_t{};
     __syncthreads();
@@ -270,10 +269,7 @@ __device__ __forceinline__ void update_small(const OrthSmallTable &t, const Orth
             const int b = p - a * (a + 1) / 2;
             float4_t sq = {};
 #pragma unroll
-            for (int c = 0; c < KB; c += KB > 1 ? 2 : 1) {
-                if constexpr (KB > 1) sq = product(A.at(a, c, lane), A.at(a, c + 1, lane), A.at(b, c, lane), A.at(b, c + 1, lane), sq);
-                else sq = product(A.at(a, c, lane), A.at(b, c, lane), sq);
-            }
+            for (int c = 0; c < KB; c += 2) sq = product(A.at(a, c, lane), A.at(a, c + 1, lane), A.at(b, c, lane), A.at(b, c + 1, lane), sq);
             // (the part itself from across the diagonal, four rows of a column side by side)
             float4_t sum = add_part(A.at(b, a, lane), st.linear, sq * st.square);
 #pragma unroll
@@ -290,10 +286,7 @@ __device__ __forceinline__ void update_small(const OrthSmallTable &t, const Orth
 #pragma unroll
             for (int i = 0; i < KB; ++i) {
 #pragma unroll
-                for (int c = 0; c < KB; c += KB > 1 ? 2 : 1) {
-                    if constexpr (KB > 1) d[i] = product(B.at(i, c, from), B.at(i, c + 1, from), x[c][j], x[c + 1][j], d[i]);
-                    else d[i] = product(B.at(i, c, from), x[c][j], d[i]);
-                }
+                for (int c = 0; c < KB; c += 2) d[i] = product(B.at(i, c, from), B.at(i, c + 1, from), x[c][j], x[c + 1][j], d[i]);
                 if (NB == 8) __builtin_amdgcn_sched_barrier(0);      // (and of B)
             }
 #pragma unroll
@@ -344,17 +337,359 @@ __device__ __forceinline__ void update_small(const OrthSmallTable &t, const Orth
     if (o.new_weight) finish_by_type(o.new_weight, o.weight, o.new_weight_stride, o.weight_dtype);
 }
 
-// KB: of the largest matrix of the launch (parts beyond a matrix are zeros, which leave its bits as they are); NB by its own columns.  LISTED: from a list in memory
-// instead of the table (a choice made on the device cost 15% of the policy network's 115 us).
-template <int KB, bool LISTED>
+// ---- up to 32 rows: over the short side, in float64
+#define INLINE __attribute__((always_inline))        // (a lambda that is left as a call would take the table of matrices to memory)
+typedef double double4_t __attribute__((ext_vector_type(4)));
+
+// 16 x 16 x 4: operands i = lane % 16, k = lane / 16; results rows 4 r + lane / 16, column lane % 16.
+__device__ __forceinline__ double4_t product(double a, double b, const double4_t &c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
+
+constexpr int kPending = 4;            // steps of a wave whose loads are on their way together
+
+template <int THIN>
+struct ThinShared {
+    static constexpr int K = THIN * 16, TILES = THIN * (THIN + 1) / 2;
+    typedef double Symmetric[K][K + 1];
+    Symmetric A;
+    union {
+        struct {
+            Symmetric B, Q[2], C;
+        };
+        double4_t added[kWaves][TILES][64];
+    };
+};
+
+// W elements of a row side by side, of which `left` are there: gradient and momentum, then what is orthogonalised.
+template <int W>
+struct Source {
+    float v[W], m[W];
+};
+
+template <typename T, int W>
+__device__ __forceinline__ void read_some(const void *p, int64_t at, int left, float (&x)[W])
+{
+    if constexpr (W == 4) load_group<T>(p, at, left, x);
+    else x[0] = left > 0 ? static_cast<float>(static_cast<const T *>(p)[at]) : 0.0f;
+}
+
+// What is orthogonalised, of a set of sources: each(f) calls f(source, row, column, left) for all of them.  FIRST: the new momentum goes to where it is
+// kept, from where the second pass takes it.
+template <bool FIRST, typename Each>
+__device__ __forceinline__ void read_all(const OrthCfg &cfg, const OrthSmall &o, Each each)
+{
+    const bool momentum = o.momentum, kept = o.new_momentum, again = !FIRST && kept;
+    if (momentum) {
+        const float *from = again ? o.new_momentum : o.momentum;
+        const int64_t stride = again ? o.new_momentum_stride : o.momentum_stride;
+        each([&](auto &x, int r, int c, int left) INLINE { read_some<float>(from, r * stride + c, left, x.m); });
+    }
+    for_type(o.grad_dtype, [&](auto type) INLINE {
+        each([&](auto &x, int r, int c, int left) INLINE { read_some<decltype(type)>(o.grad, static_cast<int64_t>(r) * o.grad_stride + c, left, x.v); });
+    });
+    if (!momentum) return;
+    each([&](auto &x, int r, int c, int left) INLINE {
+        constexpr int W = sizeof(x.v) / sizeof(float);
+#pragma unroll
+        for (int e = 0; e < W; ++e) x.m[e] = again ? x.m[e] : cfg.beta * x.m[e] + x.v[e];
+        if (FIRST && kept) {
+            const int64_t at = static_cast<int64_t>(r) * o.new_momentum_stride + c;
+            if constexpr (W == 4) store_group<float>(o.new_momentum, at, left, x.m);
+            else if (left > 0) o.new_momentum[at] = x.m[0];
+        }
+#pragma unroll
+        for (int e = 0; e < W; ++e) x.v[e] = direction(cfg, true, x.m[e], x.v[e]);
+    });
+}
+
+// Results, four side by side each, to `out` and into the weights.
+template <typename Each>
+__device__ __forceinline__ void write_all(const OrthCfg &cfg, const OrthSmall &o, Each each)
+{
+    if (o.out)
+        for_type(o.out_dtype, [&](auto type) INLINE {
+            each([&](const float (&v)[4], float (&)[4], int r, int c, int left) INLINE {
+                if (left > 0) store_group<decltype(type)>(o.out, static_cast<int64_t>(r) * o.out_stride + c, left, v);
+            });
+        });
+    if (o.new_weight)
+        for_type(o.weight_dtype, [&](auto type) INLINE {
+            typedef decltype(type) T;
+            each([&](const float (&)[4], float (&w)[4], int r, int c, int left) INLINE { load_group<T>(o.weight, static_cast<int64_t>(r) * o.weight_stride + c, left, w); });
+            each([&](const float (&v)[4], float (&w)[4], int r, int c, int left) INLINE {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = cfg.lr_decay * w[e] - cfg.lr * o.scale * v[e];
+                if (left > 0) store_group<T>(o.new_weight, static_cast<int64_t>(r) * o.new_weight_stride + c, left, w);
+            });
+        });
+}
+
+// X X' of the columns c0 .. c1 of X, 16 to a wave at a time.
+template <int THIN>
+__device__ __forceinline__ void gram_of(const OrthCfg &cfg, const OrthSmall &o, int c0, int c1, double4_t (&acc)[ThinShared<THIN>::TILES])
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, quad = lane >> 4;
+    const bool tall = o.rows > o.cols;
+    const int k = tall ? o.cols : o.rows;
+    auto add = [&](auto element) INLINE {                           // element(part of the rows, r): row r16 of it, one of four columns
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int a = 0, p = 0; a < THIN; ++a)
+#pragma unroll
+                for (int b = 0; b <= a; ++b, ++p) acc[p] = product(static_cast<double>(element(a, r)), static_cast<double>(element(b, r)), acc[p]);
+    };
+    for (int c = c0 + wave * 16; c < c1; c += kPending * kWaves * 16) {
+        if (!tall) {                                         // (a lane's four columns side by side: the order of a sum's terms is free)
+            Source<4> u[kPending][THIN];
+            auto each = [&](auto f) INLINE {
+#pragma unroll
+                for (int p = 0; p < kPending; ++p)
+#pragma unroll
+                    for (int a = 0; a < THIN; ++a) {
+                        const int row = a * 16 + r16, col = c + p * kWaves * 16 + quad * 4;
+                        f(u[p][a], row, col, row < k ? c1 - col : 0);
+                    }
+            };
+            read_all<true>(cfg, o, each);
+#pragma unroll
+            for (int p = 0; p < kPending; ++p) add([&](int a, int r) INLINE { return u[p][a].v[r]; });
+        } else {
+            Source<1> u[kPending][THIN][4];
+            auto each = [&](auto f) INLINE {
+#pragma unroll
+                for (int p = 0; p < kPending; ++p)
+#pragma unroll
+                    for (int a = 0; a < THIN; ++a)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int row = c + p * kWaves * 16 + r * 4 + quad, col = a * 16 + r16;
+                            f(u[p][a][r], row, col, row < c1 && col < k ? 1 : 0);
+                        }
+            };
+            read_all<true>(cfg, o, each);
+#pragma unroll
+            for (int p = 0; p < kPending; ++p) add([&](int a, int r) INLINE { return u[p][a][r].v[0]; });
+        }
+    }
+}
+
+// A part of X X' to both sides of the diagonal.
+template <int THIN>
+__device__ __forceinline__ void put_gram(ThinShared<THIN> &sh, int tile, int lane, const double4_t &sum)
+{
+    const int a = tile ? 1 : 0, b = tile == 2 ? 1 : 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = a * 16 + r * 4 + (lane >> 4), j = b * 16 + (lane & 15);
+        sh.A[i][j] = sum[r];
+        if (a != b) sh.A[j][i] = sum[r];
+    }
+}
+
+// From U U' in A: 1 / norm, and of the iteration on U / norm the product of all its factors.
+template <int THIN>
+__device__ __forceinline__ const typename ThinShared<THIN>::Symmetric &iterate(const OrthSmallTable &t, ThinShared<THIN> &sh, double *per_norm)
+{
+    constexpr int K = ThinShared<THIN>::K, SQ = THIN * THIN;
+    typedef typename ThinShared<THIN>::Symmetric Symmetric;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, quad = lane >> 4;
+    double trace = lane < K ? sh.A[lane % K][lane % K] : 0.0;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) trace += __shfl_xor(trace, d);
+    // nothing but zeros stays zero; a norm that is no number makes the whole matrix none
+    const double norm = sqrt(trace) + t.cfg.eps, f = norm == 0.0 ? 0.0 : norm < INFINITY ? 1.0 / norm : NAN;
+    *per_norm = f;
+    __syncthreads();
+    for (int e = tid; e < K * K; e += kWaves * 64) sh.A[e / K][e % K] *= f * f;
+    __syncthreads();
+    auto tile = [&](const Symmetric &m, const Symmetric &n, int i, int j) INLINE {
+        double4_t sum = {};
+#pragma unroll
+        for (int c = 0; c < K; c += 4) sum = product(m[i * 16 + r16][c + quad], n[j * 16 + r16][c + quad], sum);
+        return sum;
+    };
+    auto put = [&](Symmetric &to, int i, int j, const double4_t &v) INLINE {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[i * 16 + r * 4 + quad][j * 16 + r16] = v[r];
+    };
+    const int i = wave % SQ / THIN, j = wave % THIN;
+    int now = 0;
+#pragma unroll 1
+    for (int s = 0; s < t.n_steps; ++s) {
+        const double a = t.iteration[s][0], b = t.iteration[s][1], c = t.iteration[s][2];
+        const bool last = s + 1 == t.n_steps;
+        if (wave < SQ) {
+            double4_t v = tile(sh.A, sh.A, i, j);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = i * 16 + r * 4 + quad, col = j * 16 + r16;
+                v[r] = c * v[r] + b * sh.A[row][col] + (row == col ? a : 0.0);
+            }
+            put(sh.B, i, j, v);
+        }
+        __syncthreads();
+        if (wave < SQ) {
+            double4_t v;
+            if (s == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = sh.B[i * 16 + r * 4 + quad][j * 16 + r16];
+            } else {
+                v = tile(sh.B, sh.Q[now], i, j);
+            }
+            put(sh.Q[now ^ 1], i, j, v);
+        } else if (wave < 2 * SQ && !last) {
+            put(sh.C, i, j, tile(sh.B, sh.A, i, j));
+        }
+        __syncthreads();
+        if (wave < SQ && !last) put(sh.A, i, j, tile(sh.C, sh.B, i, j));
+        now ^= 1;
+        __syncthreads();
+    }
+    return sh.Q[now];
+}
+
+// The columns c0 .. c1 of Q X.  A wave reads all rows of its columns before it writes them (out may be grad).
+template <int THIN>
+__device__ __forceinline__ void apply_to(const OrthCfg &cfg, const OrthSmall &o, const typename ThinShared<THIN>::Symmetric &Q, double f, int c0, int c1)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, quad = lane >> 4;
+    const bool tall = o.rows > o.cols;
+    const int k = tall ? o.cols : o.rows;
+    double q[THIN][4][THIN];                                 // of rows [part][r] the rows [part] of the result
+    if (!tall) {
+        // X' Q: a lane has the columns 4 r16 .. of the rows 4 r + quad, and then of row r16 the columns 4 (4 r + quad) ..
+#pragma unroll
+        for (int a = 0; a < THIN; ++a)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < THIN; ++i) q[a][r][i] = Q[a * 16 + r * 4 + quad][i * 16 + r16] * f;
+        for (int c = c0 + wave * 64; c < c1; c += kWaves * 64) {
+            Source<4> u[THIN][4];
+            auto each = [&](auto g) INLINE {
+#pragma unroll
+                for (int a = 0; a < THIN; ++a)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = a * 16 + r * 4 + quad, col = c + r16 * 4;
+                        g(u[a][r], row, col, row < k ? c1 - col : 0);
+                    }
+            };
+            read_all<false>(cfg, o, each);
+#pragma unroll
+            for (int i = 0; i < THIN; ++i) {
+                double4_t d[4] = {};
+#pragma unroll
+                for (int a = 0; a < THIN; ++a)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) d[e] = product(static_cast<double>(u[a][r].v[e]), q[a][r][i], d[e]);
+                float v[4][4], w[4][4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[r][e] = static_cast<float>(d[e][r]);
+                write_all(cfg, o, [&](auto g) INLINE {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = i * 16 + r16, col = c + (r * 4 + quad) * 4;
+                        g(v[r], w[r], row, col, row < k ? c1 - col : 0);
+                    }
+                });
+            }
+        }
+    } else {
+        // Q X: a lane has the rows 4 quad .. of column r16, before and after (row 4 r + quad of a product is row 4 quad + r of the result)
+#pragma unroll
+        for (int a = 0; a < THIN; ++a)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < THIN; ++i) q[a][r][i] = Q[i * 16 + (r16 & 3) * 4 + (r16 >> 2)][a * 16 + quad * 4 + r] * f;
+        for (int c = c0 + wave * 16; c < c1; c += kPending * kWaves * 16) {
+            Source<4> u[kPending][THIN];
+            auto each = [&](auto g) INLINE {
+#pragma unroll
+                for (int p = 0; p < kPending; ++p)
+#pragma unroll
+                    for (int a = 0; a < THIN; ++a) {
+                        const int row = c + p * kWaves * 16 + r16, col = a * 16 + quad * 4;
+                        g(u[p][a], row, col, row < c1 ? k - col : 0);
+                    }
+            };
+            read_all<false>(cfg, o, each);
+            float v[kPending][THIN][4], w[kPending][THIN][4];
+#pragma unroll
+            for (int p = 0; p < kPending; ++p)
+#pragma unroll
+                for (int i = 0; i < THIN; ++i) {
+                    double4_t d = {};
+#pragma unroll
+                    for (int a = 0; a < THIN; ++a)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) d = product(q[a][r][i], static_cast<double>(u[p][a].v[r]), d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[p][i][e] = static_cast<float>(d[e]);
+                }
+            write_all(cfg, o, [&](auto g) INLINE {
+#pragma unroll
+                for (int p = 0; p < kPending; ++p)
+#pragma unroll
+                    for (int i = 0; i < THIN; ++i) {
+                        const int row = c + p * kWaves * 16 + r16, col = i * 16 + quad * 4;
+                        g(v[p][i], w[p][i], row, col, row < c1 ? k - col : 0);
+                    }
+            });
+        }
+    }
+}
+
+// The waves' sums of X X' added in their order: out(tile, lane, sum).
+template <int THIN, typename F>
+__device__ __forceinline__ void add_waves(ThinShared<THIN> &sh, const double4_t (&acc)[ThinShared<THIN>::TILES], F out)
+{
+    constexpr int TILES = ThinShared<THIN>::TILES;
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int p = 0; p < TILES; ++p) sh.added[tid >> 6][p][tid & 63] = acc[p];
+    __syncthreads();
+    for (int e = tid; e < TILES * 64; e += kWaves * 64) {
+        double4_t sum = sh.added[0][e >> 6][e & 63];
+        for (int w = 1; w < kWaves; ++w) sum += sh.added[w][e >> 6][e & 63];
+        out(e >> 6, e & 63, sum);
+    }
+    __syncthreads();
+}
+
+template <int THIN>
+__device__ __forceinline__ void update_thin(const OrthSmallTable &t, const OrthSmall &o, ThinShared<THIN> &sh)
+{
+    const int n = max(o.rows, o.cols);
+    double4_t acc[ThinShared<THIN>::TILES] = {};
+    gram_of<THIN>(t.cfg, o, 0, n, acc);
+    add_waves<THIN>(sh, acc, [&](int tile, int lane, const double4_t &sum) INLINE { put_gram<THIN>(sh, tile, lane, sum); });
+    double f;
+    const auto &Q = iterate<THIN>(t, sh, &f);
+    apply_to<THIN>(t.cfg, o, Q, f, 0, n);
+}
+
+// LISTED: from a list in memory instead of the table (a choice made on the device cost 15% of the policy network's 115 us).
+template <bool LISTED>
 __global__ __launch_bounds__(kWaves * 64) void k_orth_small(OrthSmallTable t, const OrthSmall *__restrict__ list)
 {
-    __shared__ SmallShared<KB> sh;
+    __shared__ union {
+        SmallShared of_64;
+        ThinShared<1> of_16;
+        ThinShared<2> of_32;
+    } sh;
     const OrthSmall &o = LISTED ? list[blockIdx.x] : t.m[blockIdx.x];
-    const int n = max(o.rows, o.cols);
-    if (n <= 16 * kWaves) update_small<KB, 1>(t, o, sh);
-    else if (n <= 64 * kWaves) update_small<KB, 4>(t, o, sh);
-    else update_small<KB, 8>(t, o, sh);
+    const int n = max(o.rows, o.cols), k = min(o.rows, o.cols);
+    if (k <= 16) update_thin<1>(t, o, sh.of_16);
+    else if (k <= kOrthThin) update_thin<2>(t, o, sh.of_32);
+    else if (n <= 16 * kWaves) update_small<1>(t, o, sh.of_64);
+    else if (n <= 64 * kWaves) update_small<4>(t, o, sh.of_64);
+    else update_small<8>(t, o, sh.of_64);
 }
 
 __global__ __launch_bounds__(256) void k_orth_small_list(OrthSmallTable t, OrthSmall *__restrict__ list, int at)
@@ -365,14 +700,111 @@ __global__ __launch_bounds__(256) void k_orth_small_list(OrthSmallTable t, OrthS
     for (uint32_t i = threadIdx.x; i < t.n * sizeof(OrthSmall) / 4; i += 256) to[i] = from[i];
 }
 
-// Longer ones of up to 32 rows, 16 KB.
-template <int KB, bool LISTED>
-__global__ __launch_bounds__(kWaves * 64) void k_orth_long(OrthSmallTable t, const OrthSmall *__restrict__ list)
+// ---- long ones of up to 32 rows, in parts: the parts' X X', then their sum and the iteration, then the parts' results.  A matrix' room has
+// a tile of 16 x 16 behind the other of every part's X X' (as the lanes have them), then those of the factors' product over the norm.
+struct LongPart {
+    const OrthSmall *o;
+    int part, parts, c0, c1;
+};
+
+__device__ __forceinline__ int parts_of(const OrthSmall &o, int *columns)
 {
-    __shared__ SmallShared<KB> sh;
+    const int n = max(o.rows, o.cols);
+    *columns = orth_part(n);
+    return (n + *columns - 1) / *columns;
+}
+
+// The part that a workgroup has: the last matrix whose parts begin at or in front of it.
+__device__ __forceinline__ LongPart part_of(const OrthSmall *list, int count, int id)
+{
+    int in_front = 0;
+    for (int i0 = 0; i0 < count; i0 += 64) {
+        const int i = i0 + (threadIdx.x & 63);
+        in_front += __popcll(__ballot(i < count && list[min(i, count - 1)].first <= id));
+    }
+    LongPart p;
+    p.o = list + (in_front - 1);
+    p.part = id - p.o->first;
+    int columns;
+    p.parts = parts_of(*p.o, &columns);
+    p.c0 = p.part * columns;
+    p.c1 = min(max(p.o->rows, p.o->cols), p.c0 + columns);
+    return p;
+}
+
+typedef double double4_room __attribute__((ext_vector_type(4), aligned(16)));
+
+// f(16 or 32 rows)
+template <typename F>
+__device__ __forceinline__ void by_rows(const OrthSmall &o, F f)
+{
+    if (min(o.rows, o.cols) <= 16) f(std::integral_constant<int, 1>{});
+    else f(std::integral_constant<int, 2>{});
+}
+
+union LongShared {
+    ThinShared<1> of_16;
+    ThinShared<2> of_32;
+    template <int THIN>
+    __device__ ThinShared<THIN> &get()
+    {
+        if constexpr (THIN == 1) return of_16;
+        else return of_32;
+    }
+};
+
+template <bool LISTED>
+__global__ __launch_bounds__(kWaves * 64) void k_orth_long_gram(OrthSmallTable t, const OrthSmall *__restrict__ list, int count)
+{
+    __shared__ LongShared sh;
+    const LongPart p = part_of(LISTED ? list : t.m, count, blockIdx.x);
+    by_rows(*p.o, [&](auto thin) INLINE {
+        constexpr int THIN = decltype(thin)::value, TILES = ThinShared<THIN>::TILES;
+        double4_t acc[TILES] = {};
+        gram_of<THIN>(t.cfg, *p.o, p.c0, p.c1, acc);
+        double4_room *to = static_cast<double4_room *>(p.o->room) + static_cast<int64_t>(p.part) * (TILES * 64);
+        add_waves<THIN>(sh.get<THIN>(), acc, [&](int tile, int lane, const double4_t &sum) INLINE { to[tile * 64 + lane] = sum; });
+    });
+}
+
+template <bool LISTED>
+__global__ __launch_bounds__(kWaves * 64) void k_orth_long_iterate(OrthSmallTable t, const OrthSmall *__restrict__ list)
+{
+    __shared__ LongShared sh;
     const OrthSmall &o = LISTED ? list[blockIdx.x] : t.m[blockIdx.x];
-    if (KB == 2 || max(o.rows, o.cols) <= 256 * kWaves) update_small<KB, 16>(t, o, sh);
-    else update_small<KB, 32>(t, o, sh);
+    by_rows(o, [&](auto thin) INLINE {
+        constexpr int THIN = decltype(thin)::value, TILES = ThinShared<THIN>::TILES, K = ThinShared<THIN>::K;
+        ThinShared<THIN> &mine = sh.get<THIN>();
+        int columns;
+        const int parts = parts_of(o, &columns), tid = threadIdx.x;
+        const double4_room *from = static_cast<const double4_room *>(o.room);
+        for (int e = tid; e < TILES * 64; e += kWaves * 64) {
+            double4_t sum = {};
+#pragma unroll 8
+            for (int p = 0; p < parts; ++p) sum += from[p * (TILES * 64) + e];
+            put_gram<THIN>(mine, e >> 6, e & 63, sum);
+        }
+        __syncthreads();
+        double f;
+        const auto &Q = iterate<THIN>(t, mine, &f);
+        double *to = static_cast<double *>(o.room) + static_cast<int64_t>(parts) * (TILES * 256);
+        for (int e = tid; e < K * K; e += kWaves * 64) to[e] = Q[e / K][e % K] * f;
+    });
+}
+
+template <bool LISTED>
+__global__ __launch_bounds__(kWaves * 64) void k_orth_long_apply(OrthSmallTable t, const OrthSmall *__restrict__ list, int count)
+{
+    __shared__ LongShared sh;
+    const LongPart p = part_of(LISTED ? list : t.m, count, blockIdx.x);
+    by_rows(*p.o, [&](auto thin) INLINE {
+        constexpr int THIN = decltype(thin)::value, TILES = ThinShared<THIN>::TILES, K = ThinShared<THIN>::K;
+        ThinShared<THIN> &mine = sh.get<THIN>();
+        const double *from = static_cast<const double *>(p.o->room) + static_cast<int64_t>(p.parts) * (TILES * 256);
+        for (int e = threadIdx.x; e < K * K; e += kWaves * 64) mine.A[e / K][e % K] = from[e];
+        __syncthreads();
+        apply_to<THIN>(t.cfg, *p.o, mine.A, 1.0, p.c0, p.c1);
+    });
 }
 
 }  // namespace
@@ -382,16 +814,17 @@ void launch_orth_small_list(const OrthSmallTable &t, OrthSmall *list, int at, hi
     hipLaunchKernelGGL(k_orth_small_list, dim3(1), dim3(256), 0, s, t, list, at);
 }
 
-void launch_orth_small(const OrthSmallTable &t, const OrthSmall *list, int count, int k, int n, hipStream_t s)
+void launch_orth_small(const OrthSmallTable &t, const OrthSmall *list, int count, hipStream_t s)
 {
-    const auto go = [&](auto listed) {
-        constexpr bool LISTED = decltype(listed)::value;
-        const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(count), dim3(kWaves * 64), 0, s, t, list); };
-        if (n > kOrthSmall / 64) launch(k <= 16 ? k_orth_long<1, LISTED> : k_orth_long<2, LISTED>);
-        else launch(k <= 16 ? k_orth_small<1, LISTED> : k <= 32 ? k_orth_small<2, LISTED> : k_orth_small<4, LISTED>);
-    };
-    if (list) go(std::true_type{});
-    else go(std::false_type{});
+    hipLaunchKernelGGL(list ? k_orth_small<true> : k_orth_small<false>, dim3(count), dim3(kWaves * 64), 0, s, t, list);
+}
+
+void launch_orth_long(const OrthSmallTable &t, const OrthSmall *list, int count, int parts, hipStream_t s)
+{
+    const dim3 block(kWaves * 64);
+    hipLaunchKernelGGL(list ? k_orth_long_gram<true> : k_orth_long_gram<false>, dim3(parts), block, 0, s, t, list, count);
+    hipLaunchKernelGGL(list ? k_orth_long_iterate<true> : k_orth_long_iterate<false>, dim3(count), block, 0, s, t, list);
+    hipLaunchKernelGGL(list ? k_orth_long_apply<true> : k_orth_long_apply<false>, dim3(parts), block, 0, s, t, list, count);
 }
 
 }  // namespace pl

@@ -75,11 +75,14 @@ struct OrthGrid {
     OrthWork work[3];
 };
 
-// Matrices that one workgroup does alone (kernels_orthogonal_small.hip): up to 16 x 4096, 32 x 2048 or 64 x 1024, or the other way round.
+// Matrices of few rows (kernels_orthogonal_small.hip).  Up to 16 x 4096, 32 x 2048 or 64 x 1024, or the other way round, a workgroup does
+// alone; longer ones of up to 32 rows are cut into parts.
 constexpr int kOrthSmall = 65536;
+constexpr int kOrthThin = 32;          // rows of matrices whose iteration goes over X X' alone, in float64
 inline int orth_small_k(int k) { return k <= 16 ? 16 : k <= 32 ? 32 : 64; }
-inline int orth_small_n(int n) { return n <= 128 ? 128 : n <= 512 ? 512 : n <= 1024 ? 1024 : n <= 2048 ? 2048 : 4096; }
+inline int orth_small_n(int n) { return n <= 128 ? 128 : n <= 512 ? 512 : 1024; }      // (of more than 32 rows)
 inline bool orth_small(int k, int n) { return k <= 64 && n <= kOrthSmall / orth_small_k(k); }
+inline bool orth_long(int k, int n) { return k <= kOrthThin && !orth_small(k, n); }
 constexpr int kOrthSmallListed = 24;   // matrices that go to a launch by value (a kernel's arguments end at 4 KiB); more through a list
 
 struct OrthSmall {
@@ -87,9 +90,10 @@ struct OrthSmall {
     const float *momentum;
     float *new_momentum;
     void *new_weight, *out;
-    float *room;                       // orth_room() floats
+    void *room;                        // orth_room() bytes
     uint32_t grad_stride, momentum_stride, new_momentum_stride, weight_stride, new_weight_stride, out_stride;
-    uint16_t rows, cols;
+    int32_t rows, cols;
+    int32_t first;                     // of long ones: parts of the matrices in front of it
     uint8_t grad_dtype, weight_dtype, out_dtype;
     float scale;
 };
@@ -97,22 +101,30 @@ struct OrthSmall {
 struct OrthSmallTable {
     OrthSmall m[kOrthSmallListed];
     OrthStep step[kOrthMaxSteps];
+    float iteration[kOrthMaxSteps][3];
     OrthCfg cfg;
     float x_scale, per_last;           // of the first step's X; 1 over that of the result
     int32_t n, n_steps;
 };
 static_assert(sizeof(OrthSmallTable) <= 4000, "passed by value");
 
-// Floats of a small matrix, by its columns (of 64 up to 1024 of them, where one of few rows may lie in a launch with others of 64).
+// Columns (of the longer side) of a part of a long matrix, 256 of them at most, and how many parts it has.
+__host__ __device__ inline int orth_part(int n) { return n <= 256 * 1024 ? 1024 : ((n + 255) / 256 + 63) / 64 * 64; }
+inline int orth_parts(int n) { return (n + orth_part(n) - 1) / orth_part(n); }
+
+// Bytes of a matrix: of X by columns (more than 32 rows), or of the parts' X X' and the result's factor.
 inline size_t orth_room(int rows, int cols)
 {
-    const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    return static_cast<size_t>(n <= kOrthSmall / 64 ? 64 : orth_small_k(k)) * orth_small_n(n);
+    const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows, kb = k <= 16 ? 1 : 2;
+    if (k > kOrthThin) return static_cast<size_t>(64) * orth_small_n(n) * sizeof(float);
+    if (orth_small(k, n)) return 0;
+    return (static_cast<size_t>(orth_parts(n)) * (kb * (kb + 1) / 2) + kb * kb) * 256 * sizeof(double);
 }
 
-// The table's matrices to list[at ..]; `count` matrices, by value or from a list, with sides of at most k and n.
+// The table's matrices to list[at ..]; `count` matrices by value or from a list: a workgroup each, or long ones of `parts` parts together.
 void launch_orth_small_list(const OrthSmallTable &t, OrthSmall *list, int at, hipStream_t s);
-void launch_orth_small(const OrthSmallTable &t, const OrthSmall *list, int count, int k, int n, hipStream_t s);
+void launch_orth_small(const OrthSmallTable &t, const OrthSmall *list, int count, hipStream_t s);
+void launch_orth_long(const OrthSmallTable &t, const OrthSmall *list, int count, int parts, hipStream_t s);
 void launch_orth_list(const OrthTable &t, OrthMatrix *list, int at, hipStream_t s);
 void launch_orth_start(const OrthMatrix *list, const OrthGrid &grid, const OrthCfg &cfg, float x_scale, hipStream_t s);
 void launch_orth_step(const OrthMatrix *list, const OrthGrid &grid, const OrthCfg &cfg, const OrthStep &step, int number, bool last,

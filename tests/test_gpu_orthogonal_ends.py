@@ -63,6 +63,105 @@ def test_products_are_as_near_as_those_of_fp32(shapes, draws):
         assert got <= allowed(fp32), (s, got, fp32)
 
 
+FEW = [(1, 1), (1, 7), (3, 2), (16, 16), (15, 33), (17, 17), (32, 32), (31, 97), (100, 29), (5, 3001), (16, 4095), (4096, 16), (30, 2047), (2048, 32),
+       (16, 4097), (5000, 9), (2, 20001), (32, 2049), (2049, 17), (29, 30001), (1, 300001)]
+
+
+@pytest.mark.parametrize("shape", FEW)
+def test_few_rows_lose_nothing(shape):
+    """Up to 32 rows everything is float64: the results have their last rounding alone, 2^-24 of an element, and what the products of float64 leave,
+    below 1e-9.  All together, then with 32 steps, other factors, and of low rank."""
+    import torch
+    import paper_1906_08879_amd as pl
+    rng = np.random.default_rng(shape[0] + shape[1])
+    k = min(shape)
+    g = rng.normal(0, 1, shape)
+    low = rng.normal(0, 1, (shape[0], max(1, k // 2))) @ rng.normal(0, 1, (max(1, k // 2), shape[1]))
+    for a, iteration in ((g, USUAL), (low, USUAL), (g * np.logspace(0, -5, shape[1]), USUAL), (g, ((1.5, -0.5, 0.0),) * 32), (g, ((1.0, 0.0, 0.0),)),
+                         (g, ((2.0, -1.5, 0.5),) * 9), (1e-30 * g, ((8.0, -20.0, 15.0), (3.0, -3.0, 1.0)))):
+        a = _round(a, "fp32")
+        steps = [tuple(float(np.float32(v)) for v in step) for step in iteration]
+        out = _mat(np.full(shape, 7.0), "fp32", 1, 1)
+        pl.orthogonal_update([_mat(a, "fp32", 3, 1)], out=[out], iteration=iteration, eps=0.0)
+        x = a if shape[0] >= shape[1] else a.T            # (the oracle's products are those of the columns)
+        x, _, _ = ot.orthogonal(x, iteration=steps, eps=0.0)
+        x = x if shape[0] >= shape[1] else x.T
+        assert np.linalg.norm(_host(out) - x) <= (2.0 ** -24 + 1e-9) * np.linalg.norm(x), (shape, iteration)
+
+
+def test_many_of_few_rows_through_lists():
+    """More than go by value, those of a workgroup each and those in parts; in place, with momentum."""
+    import torch
+    import paper_1906_08879_amd as pl
+    rng = np.random.default_rng(3)
+    shapes = [s for s in FEW if max(s) < 40000] * 3 + [(3, 5000 + 700 * i) for i in range(25)] + [(40, 50), (70, 80)]
+    host = [_round(rng.normal(0, 1, s), "bf16") for s in shapes]
+    grads, moments = [_mat(h, "bf16", 1, 1) for h in host], [_mat(np.zeros(s), "fp32", 2) for s in shapes]
+    weights = [torch.ones(s, device="cuda:0") for s in shapes]
+    pl.orthogonal_update(grads, moments, weights=weights, out=grads, lr=0.5, nesterov=False)
+    for h, g, m, w in zip(host, grads, moments, weights):
+        wide = h.shape[0] < h.shape[1]
+        x, _, xs = ot.orthogonal(h.T if wide else h)
+        x = x.T if wide else x
+        tol = bound(xs, USUAL, 4.0) if min(h.shape) > 32 else 2.0 ** -22 * np.linalg.norm(x)        # (factors of fp32)
+        assert np.array_equal(_host(m), h)
+        near(_host(g), x, tol, "bf16")
+        near(_host(w), 1.0 - 0.5 * x, 0.5 * tol + 4 * U * np.sqrt(x.size), "fp32")
+
+
+@pytest.mark.parametrize("shapes", [[(16, 5000), (9000, 3), (20, 30001)], [(5, 5000)] * 30 + [(30, 3000), (64, 64)]])
+def test_replays_of_long_matrices_of_few_rows(shapes):
+    import torch
+    import paper_1906_08879_amd as pl
+    grads, m, w = ([torch.randn(s, device="cuda:0") for s in shapes] for _ in range(3))
+    om, ow, out = ([torch.empty(s, device="cuda:0") for s in shapes] for _ in range(3))
+    ws = torch.empty(pl.orthogonal_workspace_bytes(shapes), dtype=torch.uint8, device="cuda:0")
+
+    def call():
+        pl.orthogonal_update(grads, m, om, w, ow, out, scales=0.5, decay=0.1, workspace=ws)
+
+    call()
+    torch.cuda.synchronize()
+    outs = om + ow + out
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        for t in outs:
+            t.fill_(3 + i)
+        ws.fill_(255 - i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, u) for t, u in zip(outs, want)), i
+        call()
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("shape", [(7, 90), (16, 4096), (90, 30), (20, 5000), (5000, 3)])
+def test_norms_of_few_rows_at_the_ends(shape):
+    """Nothing but zeros stays zero; one element that is no number makes the matrix none, and no other one."""
+    import torch
+    import paper_1906_08879_amd as pl
+    zero, out = torch.zeros(shape, device="cuda:0"), torch.full(shape, 7.0, device="cuda:0")
+    for eps in (0.0, 1e-7):
+        pl.orthogonal_update([zero], out=[out.fill_(7.0)], eps=eps)
+        assert (out == 0).all()
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        h, other, oo = torch.zeros(shape, device="cuda:0"), torch.randn((9, 9), device="cuda:0"), torch.empty((9, 9), device="cuda:0")
+        h[-1, -2] = bad
+        pl.orthogonal_update([h, other], out=[out.zero_(), oo])
+        assert torch.isnan(out).all() and torch.isfinite(oo).all()
+    for s in (1e37, 1e-40):
+        g = _round(np.random.default_rng(1).normal(0, 1, shape) * s, "fp32")
+        x = g if shape[0] >= shape[1] else g.T
+        x, _, _ = ot.orthogonal(x, iteration=[tuple(float(np.float32(v)) for v in step) for step in USUAL], eps=0.0)
+        pl.orthogonal_update([_mat(g, "fp32")], out=[out], eps=0.0)
+        x = x if shape[0] >= shape[1] else x.T
+        assert np.linalg.norm(_host(out) - x) <= (2.0 ** -24 + 1e-9) * np.linalg.norm(x)
+
+
 @pytest.mark.parametrize("rows,cols,rank", [(15, 200, 10), (60, 40, 30), (200, 150, 120), (700, 1300, 200)])
 def test_products_of_nearly_low_rank(rows, cols, rank):
     """Singular values over six orders: the smallest, and errors with them, grow most."""
@@ -82,7 +181,7 @@ def test_products_of_nearly_low_rank(rows, cols, rank):
 
 @pytest.mark.parametrize("nesterov", [0, 1])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("shape", [(1, 4), (40, 70), (60, 64), (3000, 16), (300, 129), (70, 3000)])
+@pytest.mark.parametrize("shape", [(1, 4), (40, 70), (60, 64), (3000, 16), (20, 9000), (9000, 5), (300, 129), (70, 3000)])
 def test_momentum_that_is_not_kept(shape, dtype, nesterov):
     """new_momentum NULL, of one matrix beside another whose momentum is kept: the direction is that of the new momentum, the old one stays."""
     import torch

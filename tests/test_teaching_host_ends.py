@@ -30,14 +30,16 @@ def test_scales_of_other_types(lib):  # noqa: F811
             pl.orthogonal_update([], out=[], scales=bad)
 
 
-@pytest.mark.parametrize("shape", [(1, 1), (1, 4096), (1, 4097), (1, 1 << 21), (4097, 1), (8, 50000), (5, 6000), (17, 2049), (33, 1024), (33, 1025), (64, 1024), (65, 64),
+@pytest.mark.parametrize("shape", [(1, 1), (1, 4096), (1, 4097), (1, 1 << 21), (4097, 1), (8, 50000), (5, 6000), (17, 2049), (32, 1 << 21), (33, 1024), (33, 1025), (64, 1024), (65, 64),
                                    (65, 1024), (333, 1111), (1000, 3000), (1024, 1024), (4096, 4096), (3000, 100000)])
 def test_workspace_is_as_large_as_documented(lib, shape):  # noqa: F811
-    """Sides padded to 32 count for thin matrices; small ones have rooms of a few sizes."""
+    """Sides padded to 32 where there are many rows; small matrices have rooms of a few sizes."""
     k, n = min(shape), max(shape)
     k32, n32, tiles = -(-k // 32) * 32, -(-n // 32) * 32, -(-k // 64)
     size = pl.orthogonal_workspace_bytes([shape])
-    if n <= (4096 if k <= 16 else 2048 if k <= 32 else 1024) and k <= 64:
+    if k <= 32:
+        least, most = (0, 0) if n <= (4096 if k <= 16 else 2048) else (1, 2 << 20)
+    elif k <= 64 and n <= 1024:
         least, most = 32 << 10, 256 << 10
     else:
         least = 4 * k * n32 + 8 * n * k32 + 8 * k * k32
