@@ -503,10 +503,13 @@ __device__ __forceinline__ const typename ThinShared<THIN>::Symmetric &iterate(c
     for (int e = tid; e < K * K; e += kWaves * 64) sh.A[e / K][e % K] *= f * f;
     __syncthreads();
     auto tile = [&](const Symmetric &m, const Symmetric &n, int i, int j) INLINE {
-        double4_t sum = {};
+        double4_t even = {}, odd = {};                   // (two chains of products, each half as long)
 #pragma unroll
-        for (int c = 0; c < K; c += 4) sum = product(m[i * 16 + r16][c + quad], n[j * 16 + r16][c + quad], sum);
-        return sum;
+        for (int c = 0; c < K; c += 8) {
+            even = product(m[i * 16 + r16][c + quad], n[j * 16 + r16][c + quad], even);
+            odd = product(m[i * 16 + r16][c + 4 + quad], n[j * 16 + r16][c + 4 + quad], odd);
+        }
+        return even + odd;
     };
     auto put = [&](Symmetric &to, int i, int j, const double4_t &v) INLINE {
 #pragma unroll
