@@ -14,8 +14,8 @@
 // 16 actions, in a lane's part of LDS up to 128 where there are many rows (by_lanes); the listed actions' gradients are then written once more
 // by the thread that has written them.  Few long rows, and those too long for 960 threads, take a pass for the sums and one for the
 // gradient.  A wave beside those that hold the row does the list (its float64 in their registers would spill theirs).
-// Bound by memory from some thousand logits on (lists of 64, 8192 rows of 65536 bf16: 347 us, 6.2 TB/s; 4104 rows of 50001: 157 us, 5.2), below
-// that by the list's float64 (lists of 3 of 8 fp32, 799744 rows: 32 us, where the bytes take 15).
+// Bound by memory from some thousand logits on (lists of 64, 8192 rows of 65536 bf16: 343 to 357 us on six cards, 6.0 to 6.3 TB/s; 4104 rows of 50001: 158 us, 5.2), below
+// that by the list's float64 (lists of 3 of 8 fp32, 799744 rows: 33 us, where the bytes take 15).
 #include <algorithm>
 #include <cmath>
 

@@ -12,10 +12,10 @@
 // s puts the largest number that an operand can hold at 2^14 (fp16 ends at 2^16), known on the host from the iteration's factors
 // and ||X|| <= 1; what it leaves below the last bit of lo is 2^-38 of that number.
 //
-// Bound by the matrix cores where matrices are large: 8192 x 4096 takes 5.9 ms, of which three products at the rate of the card's library
-// (1.40 PFLOP/s of fp16) would take 5.15, with 67 to 73% of the matrix cores' cycles busy; 16 of 1024 x 1024 with eight of 4096 x 1024 3.0
+// Bound by the matrix cores where matrices are large: 8192 x 4096 takes 6.0 ms, of which three products at the rate of the card's library
+// (1.40 PFLOP/s of fp16) would take 5.15, with 67 to 73% of the matrix cores' cycles busy; 16 of 1024 x 1024 with eight of 4096 x 1024 3.1
 // ms against 1.93 (53%: a tile's 32 blocks lie between a beginning and an end that nothing overlaps).  By the steps' dependence on one
-// another where they are small: 224 us for three of 1111 x 333 with others, 25 launches of 2 to 14 us.  Tiles of 64 to 256 by the sizes
+// another where they are small: 226 us for three of 1111 x 333 with others, 24 launches of 2 to 14 us.  Tiles of 64 to 256 by the sizes
 // (OrthKind).
 #include <algorithm>
 

@@ -16,7 +16,7 @@
 // transposed, exactly.  The waves' sums of X X' are added in LDS, two by two in a fixed order; A and B are kept there.
 //
 // Bound by the conversions between the two halves and fp32, beside the products, of the matrix with the most columns: the 24 matrices
-// of a policy network, up to 896 x 64, take 115 us in one launch, five iterations of 21 us; in tiles of several workgroups an iteration of
+// of a policy network, up to 896 x 64, take 114 us in one launch, five iterations of 21 us; in tiles of several workgroups an iteration of
 // 65 rows and more is three launches one behind another, of 9 to 14 us each.
 #include <algorithm>
 
